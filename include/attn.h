@@ -310,6 +310,134 @@ int attn_fwd_ws(const void* Q, const void* K, const void* V, void* O, float* LSE
                 int B, int H, int H_kv, int Nq, int Nk, int d, int causal, float softmax_scale,
                 int variant, float beta, float eps, void* stream);
 
+/*
+ * ---- Rotary positions, and attention over a cache of keys and values in 8 bits.
+ *
+ * For queries and keys that carry their positions (training and answering), and for answering: new tokens are appended to a
+ * cache, the queries of the new tokens attend to it, the weight that each cached token got is added up, and a cache that has
+ * grown past its budget is cut down to the tokens with the most of it.  The conventions at the top hold; what differs is said here.
+ * Sequences of a batch have lengths of their own, on the device, so that a captured graph serves growing sequences:
+ *   lengths  int32 [B]: tokens of sequence b that are in its cache, this call's new ones among them
+ *   counts   int32 [B] or NULL: how many of the call's N tokens (the first ones) sequence b really has; NULL: all N.  Token i of
+ *            these is at position lengths[b] - counts[b] + i of its cache.
+ * The library cannot look at them.  Whatever they hold, nothing outside the tensors is read or written: counts are taken into
+ * 0 .. N, tokens at positions below 0 or at or past `capacity` do not exist.
+ * int32 arrays are 4-byte aligned, everything else 16-byte.
+ */
+
+/*
+ * Rotary positions: the first `rot` columns (even, 2 <= rot <= d) of every row of Q [B,H,N,d] and K [B,H_kv,N,d] are rot/2 pairs, and
+ * pair i of the token at position p becomes  magnitude * (x cos - y sin, x sin + y cos)  of the angle p * frequencies[i];
+ * columns from rot on are copied.  Products in float32, rounded to bf16 once; angles in float64.
+ *   K, K_out         may both be NULL (H_kv is then ignored): Q alone.  H_kv need not divide H.
+ *   Q_out, K_out     may be Q and K themselves (with the same strides); they must not overlap otherwise
+ *   strides          12 numbers on the HOST, or NULL (all contiguous): stride_b, stride_h, stride_n of Q, K, Q_out, K_out in elements.
+ *                    Multiples of 8; inputs >= 0 (0: an expanded dimension), outputs > 0.
+ *   positions        int32, device: token n of sequence b is at positions[b * positions_stride_b + n] (stride 0: the same for all);
+ *                    NULL: n.  Any value, negative ones too.
+ *   frequencies      float64 [rot/2], device, radians per position (attn_rope_frequencies makes such a table)
+ *   interleaved      0: pairs are columns (i, i + rot/2); otherwise (2i, 2i + 1)
+ *   inverse          0: the rotation; otherwise the angles are negated, which (with the same magnitude) is its backward pass.
+ */
+int attn_rope(const void* Q, const void* K, void* Q_out, void* K_out, const long long* strides,
+              const int* positions, long long positions_stride_b, const double* frequencies,
+              int B, int H, int H_kv, int N, int d, int rot, int interleaved, float magnitude,
+              int inverse, void* stream);
+
+/*
+ * A table of frequencies, computed on the host into out[rot/2] (HOST memory): frequency i = base^(-2i/rot), brought to contexts
+ * `factor` (>= 1) times as long as the model was trained on by
+ *   ATTN_ROPE_NONE    nothing
+ *   ATTN_ROPE_LINEAR  every frequency divided by factor
+ *   ATTN_ROPE_NTK     base * factor^(rot/(rot-2)) in place of base (rot >= 4): the lowest frequency is divided by factor, the highest kept
+ *   ATTN_ROPE_YARN    by parts: with r = original_length * frequency / (2 pi) turns over the trained length, frequencies of
+ *                     r >= beta_fast are kept, those of r <= beta_slow divided by factor, those between mixed linearly in r
+ *                     ("YaRN: Efficient Context Window Extension of Large Language Models"); *magnitude = 0.1 ln(factor) + 1,
+ *                     the factor on queries and keys that goes with it.  beta_fast > beta_slow >= 0 (the paper: 32 and 1).
+ * *magnitude (may be NULL) is 1 for the others.
+ */
+#define ATTN_ROPE_NONE 0
+#define ATTN_ROPE_LINEAR 1
+#define ATTN_ROPE_NTK 2
+#define ATTN_ROPE_YARN 3
+int attn_rope_frequencies(double* out, float* magnitude, int rot, double base, int scaling, double factor,
+                          double original_length, double beta_fast, double beta_slow);
+
+/*
+ * The cache of one layer, memory of the caller's with room for `capacity` tokens (a positive multiple of 64) of each sequence and head:
+ *   K_cache  [B][H_kv][capacity][d]        8-bit codes, E4M3 (OCP 8-bit floating point; 0x7f and 0xff are NaN)
+ *   V_cache  [B][H_kv][capacity/64][d][64] the same: a block of 64 tokens holds its columns one after the other
+ *   K_scale, V_scale  float32 [B][H_kv][capacity/64]: a power of two for each block of 64 tokens of a head.
+ * A code stands for its E4M3 value times its block's scale.  Memory need not be cleared: nothing behind a sequence's last
+ * token is interpreted.  B * H_kv * capacity * d < 2^40, capacity <= 2^30.
+ */
+#define ATTN_CACHE_BLOCK 64
+
+/*
+ * New tokens, quantised into the cache: K, V bf16 [B,H_kv,N,d] (N >= 1).  With amax the largest finite magnitude among the new tokens
+ * of a block, the block's scale becomes the larger of 2^e, the least with e >= -100 and amax <= 448 * 2^e, and the scale
+ * of the tokens that are in the block already (none where the block begins with a new token); codes are rounded to nearest, ties to even.  Where
+ * the scale grows, older codes of the block are divided by what it grew by: exact but for codes that leave E4M3's normal range,
+ * which are rounded again.  NaN stays NaN, an infinity (and a magnitude over 1.75 * 2^127) becomes the largest number of its block.
+ *   strides  6 numbers on the HOST, or NULL: stride_b, stride_h, stride_n of K, V in elements; multiples of 8, >= 0
+ * Blocks without a new token are left as they are; in those that begin with one, and where the scale grew, codes behind the last token become 0.
+ */
+int attn_cache_append(const void* K, const void* V, const long long* strides, void* K_cache, void* V_cache,
+                      float* K_scale, float* V_scale, const int* lengths, const int* counts,
+                      int B, int H_kv, int N, int d, int capacity, void* stream);
+
+/*
+ * Attention of the newest queries over the cache, O = softmax(softmax_scale Q K^T) V and its row logsumexp; query head h attends
+ * to key/value head h / (H / H_kv) (ATTN_ERR_BAD_ARG if H is not a multiple of H_kv).
+ *   Q, O     bf16 [B,H,N,d];  LSE float32 [B,H,N]
+ *   causal   0: a query sees all lengths[b] tokens; otherwise query i sees those at positions <= lengths[b] - counts[b] + i (aligned
+ *            at the bottom right, as in attn_fwd_rect)
+ *   strides  6 numbers on the HOST, or NULL: stride_b, stride_h, stride_n of Q, O; multiples of 8, Q's >= 0, O's > 0
+ *   workspace  attn_cache_fwd_workspace_bytes(...) bytes, 16-byte aligned; contents on entry are ignored; free for reuse once the stream has
+ *            passed the call.  Where that is 0 it may be NULL.  Calls that can overlap in time need one each.
+ * A query that sees nothing, and queries i >= counts[b], give O = 0 and LSE = -infinity.  Scores, statistics and sums are float32, the row
+ * sum that of the float32 probabilities; these are rounded to bf16 as the operand of the product with V, and O is rounded once.  A NaN among the values of a token does not reach the queries that do not see it.  Deterministic; which float32 sums
+ * are formed in which order depends on the whole batch's lengths, as key blocks are shared out evenly over the chip.
+ */
+size_t attn_cache_fwd_workspace_bytes(int B, int H, int H_kv, int N, int d, int capacity);
+int attn_cache_fwd(const void* Q, const long long* strides, const void* K_cache, const void* V_cache,
+                   const float* K_scale, const float* V_scale, const int* lengths, const int* counts,
+                   void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                   int B, int H, int H_kv, int N, int d, int capacity, int causal, float softmax_scale,
+                   void* stream);
+
+/*
+ * The attention weight that each cached token got from the queries of an attn_cache_fwd call, added to what it had: for every
+ * position t < lengths[b] of key/value head h
+ *   weights_out[b][h][t] = weights_in[b][h][t] + sum over the group's heads and the counts[b] queries that see t of exp(S - LSE),
+ * float32 [B][H_kv][capacity]; weights of positions past the end become 0.  The call's own tokens (the last counts[b]) had
+ * none: weights_in is not read for them.  weights_in NULL: nobody had any.  weights_out may be weights_in.  Q, strides (3 numbers, of Q),
+ * lengths, counts, causal, softmax_scale as in the attn_cache_fwd call, LSE its output; rows whose LSE is -infinity add nothing.
+ * Sums in float32, deterministic.
+ */
+int attn_cache_weights(const void* Q, const long long* strides, const void* K_cache, const float* K_scale,
+                       const float* LSE, const int* lengths, const int* counts,
+                       const float* weights_in, float* weights_out,
+                       int B, int H, int H_kv, int N, int d, int capacity, int causal, float softmax_scale,
+                       void* stream);
+
+/*
+ * A cache cut down to min(lengths[b], budget) tokens of each sequence and head, in their order, in another cache (of `capacity_out` >= budget):
+ * the last `recent` tokens (0 <= recent <= budget) and, of those before them, the budget - recent with the largest weights, equal
+ * ones by position, the earliest first.  (NaN counts as larger than any number, -0 as 0.)  Sequences of at most `budget` tokens keep all.
+ * Tokens stand in new blocks, whose scales are the largest among those their tokens had; codes are multiplied by the (power of two) ratio:
+ * exact but for codes that leave E4M3's normal range.
+ *   weights      float32 [B][H_kv][capacity], of attn_cache_weights;  weights_out: float32 [B][H_kv][capacity_out] or NULL: those of the
+ *                kept tokens, then 0
+ *   kept         int32 [B][H_kv][budget]: the kept tokens' old positions, ascending, then -1
+ *   K_out ...    the new cache; must not overlap the old one.  Blocks behind the last kept token are left as they are.
+ * Afterwards the caller's lengths are min(lengths, budget).  Positions of later tokens for attn_rope go on counting from the old lengths.
+ */
+int attn_cache_evict(const void* K_cache, const void* V_cache, const float* K_scale, const float* V_scale,
+                     const float* weights, const int* lengths,
+                     void* K_out, void* V_out, float* K_scale_out, float* V_scale_out, float* weights_out, int* kept,
+                     int B, int H_kv, int d, int capacity, int capacity_out, int budget, int recent, void* stream);
+
 /* Human-readable name of an attn_status (static storage, never NULL). */
 const char* attn_status_string(int status);
 

@@ -13,6 +13,8 @@ flash       the tiled algorithms (Alg. 1, Alg. 2, Alg. 3 of the paper: online so
             tiles, the recomputing backward, the stabilised normaliser of Sec. 4), with a
             pluggable working precision and explicit bf16 rounding points
 metrics     error measures used by the parity tests (max-abs, relative L2, mean signed)
+positions   rotary positions, one pair at a time
+cache       the 8-bit cache: quantising append, attention over it, accumulated weights, eviction
 
 Pin status (see tests/test_oracle_*.py, all CPU-only):
   bf16.round_to_bf16 .......... pinned (worked addition example of Sec. 3.3.2, exhaustive

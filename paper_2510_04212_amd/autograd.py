@@ -99,3 +99,32 @@ def attention(q, k, v, causal=True, softmax_scale=None, variant=binding.MITIGATE
         if o is not None:
             return o
     return _FlashAttention.apply(q, k, v, bool(causal), float(softmax_scale), int(variant), beta, eps)
+
+
+class _Rope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, frequencies, positions, interleaved, magnitude, inverse):
+        ctx.save_for_backward(frequencies, positions)
+        ctx.args = (interleaved, magnitude, inverse)
+        return binding.attn_rope(q, k, frequencies, positions, interleaved, magnitude, inverse)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        # the rotation's transpose is the inverse rotation: the same node again, so that it can be differentiated again
+        frequencies, positions = ctx.saved_tensors
+        interleaved, magnitude, inverse = ctx.args
+        dq, dk = _Rope.apply(_aligned(dq), None if dk is None else _aligned(dk), frequencies, positions, interleaved, magnitude, not inverse)
+        return dq, dk, None, None, None, None, None
+
+
+def _aligned(t):
+    """A gradient in a layout that attn_rope takes (sum().backward() brings an expanded scalar)."""
+    fits = t.stride(3) == 1 and all(s % 8 == 0 for s in t.stride()[:3]) and t.data_ptr() % 16 == 0
+    return t if fits else t.contiguous()
+
+
+def rope(q, k=None, frequencies=None, positions=None, interleaved=False, magnitude=1.0):
+    """(q, k) with the first 2 * len(frequencies) columns rotated by their positions, differentiable in q and k; k may be absent (None
+    comes back).  frequencies, magnitude: binding.rope_frequencies(...); positions: int32 [N] or [B,N], by default 0 .. N-1.  Results are laid
+    out like q and k (any strides with a contiguous last dimension), ready for attention()."""
+    return _Rope.apply(q, k, frequencies, positions, bool(interleaved), float(magnitude), False)

@@ -6,6 +6,7 @@ There is no fallback: if the library has not been built, importing this module r
 """
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -69,6 +70,21 @@ _lib.attn_bwd_dq_delta.restype = _i
 _lib.attn_bwd_dq.restype = _i
 _lib.attn_bwd_workspace_bytes.argtypes = [_i, _i, _i, _i]
 _lib.attn_bwd_workspace_bytes.restype = _sz
+_lib.attn_rope.argtypes = [_vp] * 6 + [_ll, _vp] + [_i] * 7 + [_f, _i, _vp]
+_lib.attn_rope.restype = _i
+_d = ctypes.c_double
+_lib.attn_rope_frequencies.argtypes = [_vp, _vp, _i, _d, _i, _d, _d, _d, _d]
+_lib.attn_rope_frequencies.restype = _i
+_lib.attn_cache_append.argtypes = [_vp] * 9 + [_i] * 5 + [_vp]
+_lib.attn_cache_append.restype = _i
+_lib.attn_cache_fwd.argtypes = [_vp] * 11 + [_sz] + [_i] * 7 + [_f, _vp]
+_lib.attn_cache_fwd.restype = _i
+_lib.attn_cache_fwd_workspace_bytes.argtypes = [_i] * 6
+_lib.attn_cache_fwd_workspace_bytes.restype = _sz
+_lib.attn_cache_weights.argtypes = [_vp] * 9 + [_i] * 7 + [_f, _vp]
+_lib.attn_cache_weights.restype = _i
+_lib.attn_cache_evict.argtypes = [_vp] * 12 + [_i] * 7 + [_vp]
+_lib.attn_cache_evict.restype = _i
 _lib.attn_status_string.argtypes = [_i]
 _lib.attn_status_string.restype = ctypes.c_char_p
 _lib.attn_fwd_key_tile.argtypes = [_i]
@@ -83,7 +99,8 @@ EXPORTS = ["attn_fwd", "attn_fwd_ex", "attn_fwd_opt", "attn_delta", "attn_delta_
            "attn_bwd_dkdv", "attn_bwd_dq", "attn_bwd_dq_delta", "attn_fwd_strided", "attn_bwd_strided",
            "attn_fwd_gqa", "attn_bwd_gqa", "attn_fwd_rect", "attn_bwd_rect",
            "attn_bwd_workspace_bytes", "attn_fwd_ws", "attn_fwd_workspace_bytes",
-           "attn_status_string", "attn_fwd_key_tile"]
+           "attn_status_string", "attn_fwd_key_tile", "attn_rope", "attn_rope_frequencies", "attn_cache_append",
+           "attn_cache_fwd", "attn_cache_fwd_workspace_bytes", "attn_cache_weights", "attn_cache_evict"]
 
 
 class AttnError(RuntimeError):
@@ -460,3 +477,242 @@ def attn_bwd_rect(Q, K, V, O, dO, LSE, causal, softmax_scale, variant=STANDARD, 
                               _ptr(dV), _ptr(workspace), workspace.numel(), B, H, Nq, Nk, d,
                               int(bool(causal)), float(softmax_scale), int(variant), _stream(stream)))
     return dQ, dK, dV
+
+
+# ---- rotary positions and the 8-bit cache
+
+CACHE_BLOCK = 64
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def rope_frequencies(rot, base=10000.0, scaling="none", factor=1.0, original_length=0, beta_fast=32.0, beta_slow=1.0, device=None):
+    """(frequencies, magnitude) for attn_rope: a float64 tensor [rot/2] of radians per position on `device` (default: the current GPU),
+    and the factor on the rotated values (1 except under "yarn").  scaling: "none", "linear", "ntk" or "yarn", as attn_rope_frequencies of
+    the C ABI describes them."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {', '.join(_ROPE_SCALINGS)}")
+    out = torch.empty(max(int(rot) // 2, 1), dtype=torch.float64)
+    magnitude = ctypes.c_float()
+    _check(_lib.attn_rope_frequencies(_ptr(out), ctypes.byref(magnitude), int(rot), float(base), _ROPE_SCALINGS[scaling], float(factor),
+                                      float(original_length), float(beta_fast), float(beta_slow)))
+    return out.to("cuda" if device is None else device), magnitude.value
+
+
+def _on(device, stream, make):
+    """make() with the stream that the call will run on as the current one: its memory belongs to that stream."""
+    if stream is None or stream == torch.cuda.current_stream(device):
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _rows(t, name, device=None):
+    """Checks a CUDA bfloat16 tensor [B,H,N,d] on the current GPU with a contiguous last dimension; any other strides."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+        raise ValueError(f"{name} must be a CUDA bfloat16 tensor [B,H,N,d] whose last dimension is contiguous")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU")
+    return t.shape
+
+
+def _dense(t, name, shape, dtype, device):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}")
+    return t
+
+
+def _strides(*tensors):
+    """The host array of stride_b, stride_h, stride_n of each tensor; None where all are contiguous.  The stride of a dimension of one is
+    whatever torch says, and never used: the contiguous one, or 0, goes in its place."""
+    if all(t is None or t.is_contiguous() for t in tensors):
+        return None
+    out = []
+    for t in tensors:
+        if t is None:
+            out += [0, 0, 0]
+        elif t.is_contiguous():
+            B, H, N, d = t.shape
+            out += [H * N * d, N * d, d]
+        else:
+            out += [t.stride(i) if t.shape[i] > 1 else 8 * max(1, (t.shape[3] + 7) // 8) for i in range(3)]
+    return (ctypes.c_longlong * len(out))(*out)
+
+
+def _ptr_or_none(t):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def attn_rope(Q, K=None, frequencies=None, positions=None, interleaved=False, magnitude=1.0, inverse=False, Q_out=None, K_out=None,
+              stream=None):
+    """Q_out, K_out (None without K): the first 2 * len(frequencies) columns of queries and keys rotated by their positions.
+
+    Q [B,H,N,d], K [B,H_kv,N,d] with any strides; frequencies: rope_frequencies(...)[0]; positions: int32 [N] or [B,N], the default 0 .. N-1.
+    Outputs are new tensors laid out like the inputs, or Q_out, K_out, which may be Q and K themselves.  inverse: rotates back, which is the
+    backward pass (autograd.rope has both)."""
+    B, H, N, d = _rows(Q, "Q")
+    device = Q.device
+    H_kv = 0
+    if K is not None:
+        H_kv = _rows(K, "K")[1]
+        if (K.shape[0], K.shape[2], K.shape[3]) != (B, N, d):
+            raise ValueError("K must be [B,H_kv,N,d] with the batch, length and head size of Q")
+    if frequencies is None or frequencies.dim() != 1:
+        raise ValueError("frequencies must be a float64 tensor [rot/2]")
+    _dense(frequencies, "frequencies", frequencies.shape, torch.float64, device)
+    positions_stride = 0
+    if positions is not None:
+        if positions.dim() not in (1, 2) or positions.shape[-1] != N or (positions.dim() == 2 and positions.shape[0] != B) \
+                or positions.dtype != torch.int32 or positions.device != device or (positions.stride(-1) != 1 and N > 1):
+            raise ValueError(f"positions must be an int32 tensor [N] or [B,N] on {device} whose last dimension is contiguous")
+        positions_stride = positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+    if Q_out is None:
+        Q_out = _on(device, stream, lambda: torch.empty_like(Q))
+    if K is not None and K_out is None:
+        K_out = _on(device, stream, lambda: torch.empty_like(K))
+    for t, like, n in ((Q_out, Q, "Q_out"), (K_out, K, "K_out")):
+        if (t is None) != (like is None) or (t is not None and _rows(t, n) != like.shape):
+            raise ValueError(f"{n} must have the shape of {n[0]}")
+    if B and H:
+        _check(_lib.attn_rope(_ptr(Q), _ptr_or_none(K), _ptr(Q_out), _ptr_or_none(K_out), _strides(Q, K, Q_out, K_out),
+                              _ptr_or_none(positions), positions_stride, _ptr(frequencies), B, H, H_kv, N, d, 2 * frequencies.shape[0],
+                              int(bool(interleaved)), float(magnitude), int(bool(inverse)), _stream(stream)))
+    return Q_out, K_out
+
+
+class Cache(NamedTuple):
+    """Keys and values of one layer in 8 bits (the layout is described in include/attn.h): K [B,H_kv,capacity,d] and V
+    [B,H_kv,capacity/64,d,64] in torch.float8_e4m3fn, K_scale and V_scale float32 [B,H_kv,capacity/64]."""
+    K: torch.Tensor
+    V: torch.Tensor
+    K_scale: torch.Tensor
+    V_scale: torch.Tensor
+
+
+def cache_empty(B, H_kv, capacity, d, device=None):
+    """A Cache with room for `capacity` tokens (a multiple of 64) of each sequence and head; its contents are not initialised."""
+    if capacity <= 0 or capacity % CACHE_BLOCK:
+        raise ValueError(f"capacity must be a positive multiple of {CACHE_BLOCK}")
+    new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device="cuda" if device is None else device)
+    nb = capacity // CACHE_BLOCK
+    return Cache(new(torch.float8_e4m3fn, B, H_kv, capacity, d), new(torch.float8_e4m3fn, B, H_kv, nb, d, CACHE_BLOCK),
+                 new(torch.float32, B, H_kv, nb), new(torch.float32, B, H_kv, nb))
+
+
+def _cache_shape(cache, name="cache"):
+    B, H_kv, capacity, d = cache.K.shape
+    device = cache.K.device
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU")
+    nb = capacity // CACHE_BLOCK
+    _dense(cache.K, name + ".K", (B, H_kv, nb * CACHE_BLOCK, d), torch.float8_e4m3fn, device)
+    _dense(cache.V, name + ".V", (B, H_kv, nb, d, CACHE_BLOCK), torch.float8_e4m3fn, device)
+    _dense(cache.K_scale, name + ".K_scale", (B, H_kv, nb), torch.float32, device)
+    _dense(cache.V_scale, name + ".V_scale", (B, H_kv, nb), torch.float32, device)
+    return B, H_kv, capacity, d, device
+
+
+def _sequence_lengths(lengths, counts, B, device):
+    _dense(lengths, "lengths", (B,), torch.int32, device)
+    if counts is not None:
+        _dense(counts, "counts", (B,), torch.int32, device)
+
+
+def attn_cache_append(cache, K, V, lengths, counts=None, stream=None):
+    """Quantises the new tokens K, V [B,H_kv,N,d] (any strides) into the cache, in place.
+
+    lengths: int32 [B], the tokens of each sequence in its cache, the new ones among them; counts: int32 [B], how many of the N tokens (the
+    first ones) a sequence really has; all where absent."""
+    B, H_kv, capacity, d, device = _cache_shape(cache)
+    if _rows(K, "K") != _rows(V, "V") or (K.shape[0], K.shape[1], K.shape[3]) != (B, H_kv, d):
+        raise ValueError("K and V must be [B,H_kv,N,d] with the sequences, heads and head size of the cache")
+    _sequence_lengths(lengths, counts, B, device)
+    _check(_lib.attn_cache_append(_ptr(K), _ptr(V), _strides(K, V), _ptr(cache.K), _ptr(cache.V), _ptr(cache.K_scale), _ptr(cache.V_scale),
+                                  _ptr(lengths), _ptr_or_none(counts), B, H_kv, K.shape[2], d, capacity, _stream(stream)))
+
+
+def cache_fwd_workspace_bytes(B, H, H_kv, N, d, capacity):
+    """Workspace that attn_cache_fwd needs for this problem (0: none)."""
+    return int(_lib.attn_cache_fwd_workspace_bytes(B, H, H_kv, N, d, capacity))
+
+
+def _queries(Q, cache, name="Q"):
+    B, H_kv, capacity, d, device = _cache_shape(cache)
+    _, H, N, _ = _rows(Q, name)
+    if (Q.shape[0], Q.shape[3]) != (B, d):
+        raise ValueError(f"{name} must be [B,H,N,d] with the sequences and head size of the cache")
+    return B, H, H_kv, N, d, capacity, device
+
+
+def attn_cache_fwd(Q, cache, lengths, softmax_scale, causal=True, counts=None, O=None, LSE=None, workspace=None, stream=None):
+    """O, LSE = attention of the newest queries Q [B,H,N,d] (any strides) over the cache, their own tokens appended before: query i of
+    sequence b sees the first lengths[b] - counts[b] + i + 1 tokens (all lengths[b] without causal); one that sees nothing, or i >=
+    counts[b], gives O = 0 and LSE = -infinity.  lengths, counts: as in attn_cache_append.
+
+    workspace: a CUDA tensor of at least cache_fwd_workspace_bytes(...) bytes; allocated when absent.  Calls that may overlap in time (two
+    streams, two graphs) need one each."""
+    B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
+    _sequence_lengths(lengths, counts, B, device)
+    if O is None:
+        O = _on(device, stream, lambda: torch.empty((B, H, N, d), dtype=Q.dtype, device=device))
+    elif _rows(O, "O") != Q.shape:
+        raise ValueError("O must have the shape of Q")
+    if LSE is None:
+        LSE = _on(device, stream, lambda: torch.empty((B, H, N), dtype=torch.float32, device=device))
+    else:
+        _dense(LSE, "LSE", (B, H, N), torch.float32, device)
+    need = cache_fwd_workspace_bytes(B, H, H_kv, N, d, capacity)
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.device != device:
+            raise ValueError(f"workspace must be a contiguous tensor on {device}")
+        need = workspace.numel() * workspace.element_size()
+    elif need > 0:
+        workspace = _on(device, stream, lambda: torch.empty(need, dtype=torch.uint8, device=device))
+    _check(_lib.attn_cache_fwd(_ptr(Q), _strides(Q, O), _ptr(cache.K), _ptr(cache.V), _ptr(cache.K_scale), _ptr(cache.V_scale),
+                               _ptr(lengths), _ptr_or_none(counts), _ptr(O), _ptr(LSE), _ptr_or_none(workspace), need, B, H, H_kv, N, d,
+                               capacity, int(bool(causal)), float(softmax_scale), _stream(stream)))
+    return O, LSE
+
+
+def attn_cache_weights(Q, cache, LSE, lengths, softmax_scale, causal=True, counts=None, weights=None, out=None, stream=None):
+    """The attention weight each cached token got from the queries of an attn_cache_fwd call (same Q, cache, lengths, softmax_scale, causal,
+    counts; LSE its result), summed over those queries and the heads that share the token, added to `weights`: float32 [B,H_kv,capacity].
+
+    weights: what tokens got before (the call's own tokens had none: not read for them); None: nothing.  out: where the result goes, `weights`
+    itself for instance; a new tensor when absent.  Positions past a sequence's end become 0."""
+    B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
+    _sequence_lengths(lengths, counts, B, device)
+    _dense(LSE, "LSE", (B, H, N), torch.float32, device)
+    shape = (B, H_kv, capacity)
+    if weights is not None:
+        _dense(weights, "weights", shape, torch.float32, device)
+    out = _on(device, stream, lambda: torch.empty(shape, dtype=torch.float32, device=device)) if out is None else \
+        _dense(out, "out", shape, torch.float32, device)
+    _check(_lib.attn_cache_weights(_ptr(Q), _strides(Q), _ptr(cache.K), _ptr(cache.K_scale), _ptr(LSE), _ptr(lengths), _ptr_or_none(counts),
+                                   _ptr_or_none(weights), _ptr(out), B, H, H_kv, N, d, capacity, int(bool(causal)), float(softmax_scale),
+                                   _stream(stream)))
+    return out
+
+
+def attn_cache_evict(cache, weights, lengths, budget, recent, out=None, stream=None):
+    """(out, weights_out, kept): the cache cut down to min(lengths, budget) tokens of each sequence and head, the last `recent` and, of those
+    before, the ones with the largest weights (equal ones: the earliest), in their order.
+
+    weights: float32 [B,H_kv,capacity] of attn_cache_weights.  out: another Cache with room for `budget` tokens; a new one of the least
+    capacity when absent.  weights_out: float32 [B,H_kv,capacity of out], the kept tokens' weights, then 0.  kept: int32
+    [B,H_kv,budget], their old positions, then -1.  The caller's lengths are then lengths.clamp(max=budget)."""
+    B, H_kv, capacity, d, device = _cache_shape(cache)
+    _dense(weights, "weights", (B, H_kv, capacity), torch.float32, device)
+    _sequence_lengths(lengths, None, B, device)
+    if budget < 1:
+        raise ValueError("budget must be positive")
+    if out is None:
+        out = _on(device, stream, lambda: cache_empty(B, H_kv, -(-budget // CACHE_BLOCK) * CACHE_BLOCK, d, device))
+    Bo, Ho, capacity_out, do, device_out = _cache_shape(out, "out")
+    if (Bo, Ho, do, device_out) != (B, H_kv, d, device):
+        raise ValueError("out must have the sequences, heads and head size of the cache")
+    weights_out = _on(device, stream, lambda: torch.empty((B, H_kv, capacity_out), dtype=torch.float32, device=device))
+    kept = _on(device, stream, lambda: torch.empty((B, H_kv, budget), dtype=torch.int32, device=device))
+    _check(_lib.attn_cache_evict(_ptr(cache.K), _ptr(cache.V), _ptr(cache.K_scale), _ptr(cache.V_scale), _ptr(weights), _ptr(lengths),
+                                 _ptr(out.K), _ptr(out.V), _ptr(out.K_scale), _ptr(out.V_scale), _ptr(weights_out), _ptr(kept), B, H_kv, d,
+                                 capacity, capacity_out, int(budget), int(recent), _stream(stream)))
+    return out, weights_out, kept

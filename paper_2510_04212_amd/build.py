@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libattn_gfx950.so")
 PROBE_LIB = os.path.join(HERE, "libattn_probe_gfx950.so")
 NODE_LIB = os.path.join(HERE, "_autograd.so")
-SOURCES = ["api.hip", "fwd.hip", "delta.hip", "bwd.hip"]
+SOURCES = ["api.hip", "fwd.hip", "delta.hip", "bwd.hip", "api_cache.hip", "rope.hip", "cache.hip", "cache_attn.hip"]
 PROBE_SOURCES = ["probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -34,7 +34,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # (kPlacedReads in fwd.hip).  Same bits; us, without the flag -> with it: B2 H8 N2048 d256 causal 87.4 -> 72.6, B4 H8 N1999
 # 117 -> 100, B2 H12 N300 21.2 -> 18.5, full B2 H8 N2048 98.9 -> 82.7, N2000 102 -> 85; smaller head sizes as before.
 # The backward loses by it (dK/dV B2 H8 N2048 122 -> 131, dQ even).
-EXTRA_FLAGS = {"bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"], "fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA_FLAGS = {"bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"], "fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+               "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _node_command():

@@ -1,0 +1,149 @@
+"""Rotary positions (attn_rope, autograd.rope) against the 64-bit oracle.
+
+Tolerance of an element u = m (x c - y s): one bf16 rounding (2^-8 of u) and float32 work: the fraction of a turn rounded to float32
+(2^-25 of a turn at most, 2 pi 2^-25 = 1.9e-7 rad), sine and cosine (4 ulp, 2.4e-7), three products and a sum (2^-24 each): below
+1e-6 m (|x| + |y|)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import positions as oracle
+from paper_2510_04212_amd import autograd
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _draw(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).to(DEV)
+
+
+def _check(got, x, pos, freq, interleaved, magnitude=1.0, inverse=False, label=""):
+    x = x.detach().double().cpu().numpy()
+    want = oracle.rotate(x, pos, freq, interleaved, magnitude, inverse)
+    u, v = oracle.pairs(2 * len(freq), interleaved)
+    size = np.zeros_like(x)
+    size[..., u] = size[..., v] = np.abs(x[..., u]) + np.abs(x[..., v])
+    got = got.detach().double().cpu().numpy()
+    off = np.abs(got - want) - (2.0 ** -8 * np.abs(want) * (size > 0) + 1e-6 * abs(magnitude) * size)
+    assert off.max() <= 0, (label, off.max(), np.unravel_index(off.argmax(), off.shape))
+    assert np.array_equal(got[..., 2 * len(freq):], x[..., 2 * len(freq):]), label
+
+
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("d,rot", [(32, 32), (32, 8), (64, 64), (64, 32), (64, 6), (96, 96), (96, 24), (128, 128), (128, 64), (128, 2),
+                                   (128, 22), (256, 256), (256, 64), (256, 250)])
+def test_against_the_oracle(lib, d, rot, interleaved):
+    for B, H, Hkv, N in ((2, 3, 3, 37), (3, 8, 2, 1), (1, 5, 1, 130)):
+        q, k = _draw(1, B, H, N, d), _draw(2, B, Hkv, N, d)
+        pos = torch.randint(-1000, 100000, (B, N), generator=torch.Generator().manual_seed(3), dtype=torch.int32)
+        f, m = lib.rope_frequencies(rot, 10000.0, device=DEV)
+        want, _ = oracle.frequencies(rot)
+        assert m == 1.0 and np.allclose(f.cpu().numpy(), want, rtol=1e-14, atol=0)
+        a, b = lib.attn_rope(q, k, f, positions=pos.to(DEV), interleaved=interleaved, magnitude=1.25)
+        _check(a, q, pos.numpy(), want, interleaved, 1.25, label="q")
+        _check(b, k, pos.numpy(), want, interleaved, 1.25, label="k")
+        # no positions: 0 .. N-1; one row of positions for all sequences; queries alone
+        a, b = lib.attn_rope(q, k, f, interleaved=interleaved, inverse=True)
+        _check(a, q, np.tile(np.arange(N), (B, 1)), want, interleaved, inverse=True, label="q, 0 ..")
+        c, none = lib.attn_rope(q, None, f, positions=torch.arange(N, dtype=torch.int32, device=DEV), interleaved=interleaved, inverse=True)
+        assert none is None and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("scaling,factor", [("linear", 4.0), ("ntk", 16.0), ("yarn", 32.0)])
+def test_scaled_frequencies_and_far_positions(lib, scaling, factor):
+    f, m = lib.rope_frequencies(128, 10000.0, scaling, factor, original_length=4096, device=DEV)
+    want, magnitude = oracle.frequencies(128, 10000.0, scaling, factor, 4096)
+    assert np.allclose(f.cpu().numpy(), want, rtol=1e-13, atol=0) and abs(m - magnitude) < 1e-6
+    q = _draw(4, 1, 2, 9, 128)
+    pos = torch.tensor([[0, 1, 4095, 131071, 1 << 20, (1 << 24) + 1, 2 ** 31 - 1, -2 ** 31, -1]], dtype=torch.int32)
+    # 2^31 radians in float64: 2^-22 of a radian lost in the product, and as much in the oracle's: 5e-7, on top of the 1e-6
+    got, _ = lib.attn_rope(q, None, f, positions=pos.to(DEV), magnitude=m)
+    near = pos[0].abs() < 1 << 25
+    _check(got[:, :, near], q[:, :, near], pos[:, near].numpy(), f.cpu().numpy(), False, m)
+    w = oracle.rotate(q.double().cpu().numpy(), pos.numpy(), f.cpu().numpy(), False, m)
+    assert np.abs(got.double().cpu().numpy() - w).max() <= 2.0 ** -8 * np.abs(w).max() + 1e-5
+
+
+def test_layouts_in_place_and_bits_that_pass(lib):
+    """Views into a fused projection, [B,N,H,d] outputs, expanded inputs and in-place calls give the bits of contiguous ones; columns
+    behind rot keep theirs, whatever they are."""
+    B, H, Hkv, N, d, rot = 2, 6, 2, 45, 96, 40
+    x = _draw(5, B, N, H + 2 * Hkv, d)
+    x[0, 3, 1, rot:] = float("inf")
+    x[1, 7, 0, rot + 3] = float("nan")
+    x[1, 7, 0, rot + 5] = -0.0
+    q, k = x[:, :, :H].permute(0, 2, 1, 3), x[:, :, H:H + Hkv].permute(0, 2, 1, 3)
+    f, _ = lib.rope_frequencies(rot, 500.0, device=DEV)
+    bits = lambda t: t.contiguous().view(torch.int16)
+    for interleaved in (False, True):
+        want = lib.attn_rope(q.contiguous(), k.contiguous(), f, interleaved=interleaved)
+        got = lib.attn_rope(q, k, f, interleaved=interleaved)
+        assert got[0].stride() == torch.empty_like(q).stride() != want[0].stride()
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want))
+        assert torch.equal(bits(want[0][..., rot:]), bits(q[..., rot:]))
+        y = x.clone()
+        q2, k2 = y[:, :, :H].permute(0, 2, 1, 3), y[:, :, H:H + Hkv].permute(0, 2, 1, 3)
+        lib.attn_rope(q2, k2, f, interleaved=interleaved, Q_out=q2, K_out=k2)
+        assert torch.equal(bits(q2), bits(want[0])) and torch.equal(bits(k2), bits(want[1]))
+        assert torch.equal(bits(y[:, :, H + Hkv:]), bits(x[:, :, H + Hkv:]))          # V's part of the projection
+    one = _draw(6, 1, 1, N, d).expand(B, H, N, d)
+    got, _ = lib.attn_rope(one, None, f)
+    want, _ = lib.attn_rope(one.contiguous(), None, f)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("interleaved", (False, True))
+def test_gradients(lib, interleaved):
+    B, H, Hkv, N, d, rot = 2, 4, 2, 33, 64, 48
+    q, k = _draw(7, B, H, N, d).requires_grad_(), _draw(8, B, Hkv, N, d).requires_grad_()
+    pos = torch.randint(0, 5000, (B, N), dtype=torch.int32, generator=torch.Generator().manual_seed(9))
+    f, m = lib.rope_frequencies(rot, scaling="yarn", factor=4.0, original_length=1024, device=DEV)
+    freq = f.cpu().numpy()
+    gq, gk = _draw(10, B, H, N, d), _draw(11, B, Hkv, N, d).permute(0, 1, 3, 2).contiguous().permute(0, 1, 3, 2)     # rows not contiguous
+    a, b = autograd.rope(q, k, f, pos.to(DEV), interleaved, m)
+    dq, dk = torch.autograd.grad((a, b), (q, k), (gq, gk), create_graph=False)
+    _check(a, q, pos.numpy(), freq, interleaved, m)
+    _check(dq, gq, pos.numpy(), freq, interleaved, m, inverse=True, label="dq")
+    _check(dk, gk, pos.numpy(), freq, interleaved, m, inverse=True, label="dk")
+    # against differences of the oracle (linear: exact for any step)
+    e = np.random.default_rng(1).standard_normal(q.shape)
+    base = q.detach().double().cpu().numpy()
+    change = ((oracle.rotate(base + e, pos.numpy(), freq, interleaved, m) - oracle.rotate(base, pos.numpy(), freq, interleaved, m))
+              * gq.double().cpu().numpy()).sum()
+    along = (dq.double().cpu().numpy() * e).sum()
+    # sum of n roundings of size 2^-8 |dq e|, independent: 6 standard deviations
+    assert abs(change - along) <= 6 * 2.0 ** -8 * np.sqrt(((dq.double().cpu().numpy() * e) ** 2).sum()) + 1e-4
+    # only one of the two used, an expanded incoming gradient, and the gradient of the gradient
+    a, b = autograd.rope(q, k, f, pos.to(DEV), interleaved, m)
+    (s,) = torch.autograd.grad(b.sum(), (k,))
+    _check(s, torch.ones_like(k), pos.numpy(), freq, interleaved, m, inverse=True)
+    w = gq.clone().requires_grad_()
+    a, none = autograd.rope(q, None, f, pos.to(DEV), interleaved, m)
+    assert none is None
+    (g1,) = torch.autograd.grad(a, q, w, create_graph=True)
+    (g2,) = torch.autograd.grad(g1, w, q.detach())
+    _check(g2, q, pos.numpy(), freq, interleaved, m, label="second")
+
+
+def test_other_streams_and_graphs(lib):
+    q, k = _draw(12, 2, 4, 70, 128), _draw(13, 2, 2, 70, 128)
+    pos = torch.arange(70, dtype=torch.int32, device=DEV).expand(2, 70)
+    f, _ = lib.rope_frequencies(128, device=DEV)
+    want = lib.attn_rope(q, k, f, positions=pos)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = lib.attn_rope(q, k, f, positions=pos, stream=side)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    at, x = pos.contiguous(), q.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = lib.attn_rope(x, k, f, positions=at)
+    for step in range(3):
+        at.copy_(pos + 100 * step)
+        x.copy_(q * (step + 1))
+        graph.replay()
+        eager = lib.attn_rope(x, k, f, positions=at)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
