@@ -20,6 +20,7 @@
 namespace {
 
 constexpr int kThreads = 256;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 // d = 32 c + 8 half + ... of the columns: 16-byte chunks serve 64 columns (lane group g: 16 g ..), an 8-byte one the last 32 (8 g ..)
 template <int D> struct Cols {
@@ -36,26 +37,65 @@ DEVI bf16x8 widen8(unsigned lo, unsigned hi, float scale) {
   return u.v;
 }
 
-// K codes of one lane for a block: 4 tiles of 16 tokens
+// Codes of one lane for a block, 16 bytes (or 8: the last 32 columns of d = 32, 96) each: K's of tile i, columns 64 c ..; V's of column tile dt.
+// From memory into registers: every wave reads its own blocks.  K + V: 2 d registers / 8.
 template <int D> struct KCodes {
   u32x4 c[4][Cols<D>::C64 ? Cols<D>::C64 : 1];
-  uint2 odd[4];
-  // at: the block's first byte + the lane's offset (key_offset)
-  DEVI void load(const unsigned char* at, int g) {
+  u32x2 odd[4];
+  // block: its first byte, the same in all lanes; at: the lane's offset
+  DEVI void load(const unsigned char* block, unsigned at, unsigned at_odd) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int k = 0; k < Cols<D>::C64; ++k) c[i][k] = *reinterpret_cast<const u32x4*>(at + i * 4 * D + k * 64 + g * 16);
-      if constexpr (Cols<D>::ODD) odd[i] = *reinterpret_cast<const uint2*>(at + i * 4 * D + Cols<D>::C64 * 64 + g * 8);
+      for (int k = 0; k < Cols<D>::C64; ++k) c[i][k] = *reinterpret_cast<const u32x4*>(block + at + (i * 4 * D + k * 64));
+      if constexpr (Cols<D>::ODD) odd[i] = *reinterpret_cast<const u32x2*>(block + at_odd + (i * 4 * D + Cols<D>::C64 * 64));
     }
   }
-  // fragment k (of KC) of tile i
-  DEVI bf16x8 frag(int i, int k, float scale) const {
-    if (k < 2 * Cols<D>::C64) return (k & 1) ? widen8(c[i][k / 2][2], c[i][k / 2][3], scale) : widen8(c[i][k / 2][0], c[i][k / 2][1], scale);
-    return widen8(odd[i].x, odd[i].y, scale);
+  DEVI u32x4 whole(int i, int k) const { return c[i][k]; }
+  DEVI u32x2 rest(int i) const { return odd[i]; }
+};
+template <int D> struct VCodes {
+  u32x4 c[D / 16];
+  DEVI void load(const unsigned char* block, unsigned at) {
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) c[dt] = *reinterpret_cast<const u32x4*>(block + at + dt * 1024);
+  }
+  DEVI u32x4 operator()(int dt) const { return c[dt]; }
+};
+// From LDS, where a block's codes are shared by the four waves of a work-group.  Pieces of 1 KB, one transfer instruction each: 16 rows (tokens of
+// a tile, or columns of V) x 64 bytes, the four 16-byte chunks of row r permuted by slot_mask(r / 4) (common.hpp: 16 lanes reading
+// chunk g of 16 rows then meet all banks once); two tiles' 32 bytes a row for the last columns of d = 32, 96.
+template <int D> struct Staged {
+  static constexpr int KP = 4 * Cols<D>::C64 + (Cols<D>::ODD ? 2 : 0), PIECES = KP + D / 16;
+  static constexpr int kBytes = PIECES * 1024;
+  // the byte of the block that lane `lane` of piece i fetches, K's (i < KP) and V's
+  static DEVI unsigned source(int i, int lane) {
+    if (i < 4 * Cols<D>::C64) {
+      const int r = lane >> 2, tile = i / (Cols<D>::C64 ? Cols<D>::C64 : 1), c = i % (Cols<D>::C64 ? Cols<D>::C64 : 1);
+      return (unsigned)(((r >> 2) * 16 + tile * 4 + (r & 3)) * D + c * 64 + (((lane & 3) ^ slot_mask(r >> 2)) << 4));
+    }
+    if (i < KP) {
+      const int r = (lane >> 1) & 15, tile = 2 * (i - 4 * Cols<D>::C64) + (lane >> 5);
+      return (unsigned)(((r >> 2) * 16 + tile * 4 + (r & 3)) * D + Cols<D>::C64 * 64 + ((lane & 1) << 4));
+    }
+    const int r = lane >> 2;
+    return (unsigned)(((i - KP) * 16 + r) * kBlock + (((lane & 3) ^ slot_mask(r >> 2)) << 4));
   }
 };
-DEVI int key_offset(int r, int D) { return ((r >> 2) * 16 + (r & 3)) * D; }
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) const u32x2 lds_uint2;
+template <int D> struct StagedBlock {
+  int at, at_odd;                       // LDS addresses: the buffer's + the lane's
+  DEVI u32x4 whole(int i, int k) const { return *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (i * Cols<D>::C64 + k) * 1024)); }
+  DEVI u32x2 rest(int i) const { return *reinterpret_cast<lds_uint2*>((unsigned long)(unsigned)(at_odd + 4 * Cols<D>::C64 * 1024 + i * 512)); }
+  DEVI u32x4 operator()(int dt) const { return *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (Staged<D>::KP + dt) * 1024)); }
+};
+// 64 lanes' 16 bytes each from block + at into LDS at `to` .. + 1023; `block` and `to` the same in all lanes.  Inline assembly as in common.hpp's
+// TileLoader, and for its reasons; waited for with wait_vmem().
+DEVI void fetch_piece(const unsigned char* block, unsigned at, unsigned to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(block) : "m0");
+}
+DEVI bf16x8 key_frag(const u32x4& w, int half, float scale) { return widen8(w[2 * half], w[2 * half + 1], scale); }
 
 // the columns of a query row that go with fragment k: 8 consecutive from here
 template <int D> DEVI int query_column(int k, int g) {
@@ -131,133 +171,140 @@ template <int D, int RT> struct Acc {
 };
 template <int D, int RT, int KW> constexpr int kSlotFloats = (4 / KW) * RT * (D / 16 * 256 + 32);
 
-template <int RT> struct RowsOf {
-  int row[RT], query[RT], head[RT];       // row < 0: none
-  int limit[RT];                          // tokens it sees; no row: all, so that it asks for no masking
-  bool empty[RT];                         // a row whose output is 0
+// A row of the list: which query and head it is, and how many tokens it sees.
+struct Row {
+  int query, head, limit;
+  bool there, empty;                    // empty: its output is 0
 };
-
-// O and LSE of row r of tile rt, from the sum and the maximum
-template <int D, int RT>
-DEVI void store_rows(const AttendArgs& p, const RowsOf<RT>& rows, int b, int h, Acc<D, RT>& a, int g) {
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    if (rows.row[rt] < 0) continue;
-    const int head = h * p.group + rows.head[rt];
-    unsigned short* to = p.O + b * p.o_sb + head * p.o_sh + rows.query[rt] * p.o_sn;
-    const float l = a.l[rt];
-    const Divisor by = make_divisor(l);
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) {
-      union { bf16x4 v; uint2 w; } u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) u.v[i] = rows.empty[rt] ? (bf16_t)0.f : (bf16_t)divide(a.o[rt][dt][i], by);
-      *reinterpret_cast<uint2*>(to + dt * 16 + g * 4) = u.w;
-    }
-    if (g == 0)
-      p.LSE[((size_t)b * p.H + head) * p.N + rows.query[rt]] = rows.empty[rt] ? -INFINITY : (a.m[rt] + log2f(l)) * 0.6931471805599453f;
-  }
-}
-template <int RT>
-DEVI void find_rows(RowsOf<RT>& rows, const AttendArgs& p, int b, int first, int r) {
+DEVI Row find_row(const AttendArgs& p, int b, int row) {
   const int n = real_count(p.counts, b, p.N);
   const long long length = p.lengths[b];
   const long long all = max(0ll, min(length, (long long)p.cache.capacity));
+  Row x;
+  x.there = row < p.N * p.group;
+  x.query = x.there ? row / p.group : 0;
+  x.head = x.there ? row - x.query * p.group : 0;
+  const long long seen = p.causal ? min(all, length - n + x.query + 1) : all;
+  x.empty = x.query >= n || seen <= 0;
+  x.limit = x.there && x.query < n ? (int)max(0ll, seen) : 0x7fffffff;       // a row that nobody asks for needs no masking
+  return x;
+}
+// O and LSE of a row: DT column tiles from dt0 on
+template <int DT>
+DEVI void store_row(const AttendArgs& p, const Row& x, int b, int h, const f32x4* o, float m, float l, int dt0, int g) {
+  if (!x.there) return;
+  const int head = h * p.group + x.head;
+  unsigned short* to = p.O + b * p.o_sb + head * p.o_sh + x.query * p.o_sn + dt0 * 16 + g * 4;
+  const Divisor by = make_divisor(l);
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int row = first + rt * 16 + r;
-    const bool there = row < p.N * p.group;
-    const int query = there ? row / p.group : 0;
-    rows.row[rt] = there ? row : -1;
-    rows.query[rt] = query;
-    rows.head[rt] = there ? row - query * p.group : 0;
-    const long long seen = p.causal ? min(all, length - n + query + 1) : all;
-    rows.empty[rt] = there && (query >= n || seen <= 0);
-    rows.limit[rt] = there && query < n ? (int)max(0ll, seen) : 0x7fffffff;
+  for (int i = 0; i < DT; ++i) {
+    union { bf16x4 v; u32x2 w; } u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) u.v[c] = x.empty ? (bf16_t)0.f : (bf16_t)divide(o[i][c], by);
+    *reinterpret_cast<u32x2*>(to + i * 16) = u.w;
   }
+  if (dt0 == 0 && g == 0) p.LSE[((size_t)b * p.H + head) * p.N + x.query] = x.empty ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // bytes of w that are 0x7f or 0xff, E4M3's NaN: 0x80 in each of them
 DEVI unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-// A masked block whose V holds NaN: 0 * NaN must not reach the rows that do not see that token.  The codes are cleared, and an
+DEVI u32x4 without_nan(u32x4 w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] &= ~((nan_codes(w[i]) >> 7) * 0xffu);
+  return w;
+}
+
+// A masked block: does its V hold NaN?  0 * NaN must not reach the rows that do not see that token, so its codes count as 0 then, and an
 // output to which a row's visible tokens bring a NaN is made one: that count is a product, too, of ones.
-template <int D, int RT>
-DEVI void take_out_nan(Acc<D, RT>& a, u32x4 (&v)[D / 16], const RowsOf<RT>& rows, int t0, int g) {
-  bf16x8 seen[RT][2];
+template <int D, int RT, class V>
+DEVI bool take_out_nan(Acc<D, RT>& a, const V& v, const int (&limit)[RT], int t0, int g) {
+  bool any = false;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) seen[rt][j][e] = (bf16_t)(t0 + 16 * g + 8 * j + e < rows.limit[rt] ? 1.f : 0.f);
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt)
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const u32x4 w = v(dt);
+    const unsigned bad = nan_codes(w[0]) | nan_codes(w[1]) | nan_codes(w[2]) | nan_codes(w[3]);
+    if (!__any(bad != 0)) continue;
+    any = true;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const unsigned lo = nan_codes(v[dt][2 * j]), hi = nan_codes(v[dt][2 * j + 1]);
-      bf16x8 bad;
+      const unsigned lo = nan_codes(w[2 * j]), hi = nan_codes(w[2 * j + 1]);
+      bf16x8 ones;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) bad[e] = (bf16_t)((((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0x80u) ? 1.f : 0.f);
-      v[dt][2 * j] &= ~((lo >> 7) * 0xffu);
-      v[dt][2 * j + 1] &= ~((hi >> 7) * 0xffu);
+      for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)((((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0x80u) ? 1.f : 0.f);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        f32x4 count{0, 0, 0, 0};
-        count = mfma16(bad, seen[rt][j], count);
+        bf16x8 seen;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) seen[e] = (bf16_t)(t0 + 16 * g + 8 * j + e < limit[rt] ? 1.f : 0.f);
+        const f32x4 count = mfma16(ones, seen, f32x4{0, 0, 0, 0});
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (count[i] > 0.f) a.o[rt][dt][i] = NAN;
       }
     }
+  }
+  return any;
 }
 
 // One block of 64 tokens for a wave's rows.  masked (the same in all lanes): some row does not see all of it.  after_scores() is called when
 // K's codes have been used.
-template <int D, int RT, class F>
-DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, u32x4 (&v)[D / 16], float k_scale, float v_scale,
-                     float scale_log2, const RowsOf<RT>& rows, bool masked, int t0, int g, F&& after_scores) {
+//
+// The maximum that probabilities are taken relative to is let fall behind the true one by up to kSlack (a factor of 2^kSlack, harmless in float32 and
+// bf16 alike), so that the accumulators are hardly ever rescaled.
+constexpr float kSlack = 8.f;
+template <int D, int RT, class K, class V, class F>
+DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, const V& v, float k_scale, float v_scale, float scale_log2,
+                     const int (&limit)[RT], bool masked, int t0, int g, F&& after_scores) {
   f32x4 s[RT][4];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[rt][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      const bf16x8 kf = k.frag(i, c, k_scale);
+    for (int c = 0; c < Cols<D>::C64; ++c) {
+      const u32x4 w = k.whole(i, c);
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][c], s[rt][i]);
+      for (int half = 0; half < 2; ++half) {
+        const bf16x8 kf = key_frag(w, half, k_scale);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][2 * c + half], s[rt][i]);
+      }
     }
+    if constexpr (Cols<D>::ODD) {
+      const u32x2 w = k.rest(i);
+      const bf16x8 kf = widen8(w.x, w.y, k_scale);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][D / 32 - 1], s[rt][i]);
+    }
+  }
   after_scores();
+  bool nan = false;
   if (masked) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int seen = rows.limit[rt] - t0 - 16 * g;
+      const int seen = limit[rt] - t0 - 16 * g;
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (i >= seen) s[rt][i / 4][i % 4] = -INFINITY;
     }
-    bool bad = false;
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= nan_codes(v[dt][i]) != 0;
-    if (__any(bad)) take_out_nan<D, RT>(a, v, rows, t0, g);
+    nan = take_out_nan<D, RT>(a, v, limit, t0, g);
   }
   bf16x8 pr[RT][2];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float most = -INFINITY;
+    float most = s[rt][0][0];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) most = fmaxf(most, s[rt][i / 4][i % 4]);
-    const float m = fmaxf(a.m[rt], max_over_groups(most) * scale_log2);
-    const float use = m == -INFINITY ? 0.f : m;            // nothing seen so far: exp2(-inf) = 0
-    if (__any(m != a.m[rt])) {
-      a.scale(rt, __builtin_amdgcn_exp2f(a.m[rt] - use));
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[rt][i / 4][i % 4]);
+    most = max_over_groups(most) * scale_log2;
+    if (__any(most > a.m[rt] + kSlack)) {
+      const float m = most > a.m[rt] + kSlack ? most : a.m[rt];
+      a.scale(rt, __builtin_amdgcn_exp2f(a.m[rt] - (m == -INFINITY ? 0.f : m)));
       a.m[rt] = m;
     }
+    const float use = a.m[rt] == -INFINITY ? 0.f : a.m[rt];            // nothing seen so far: exp2(-inf) = 0
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -268,22 +315,30 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
       }
   }
 #pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt)
+  for (int dt = 0; dt < D / 16; ++dt) {
+    u32x4 w = v(dt);
+    if (nan) w = without_nan(w);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const bf16x8 vf = widen8(v[dt][2 * j], v[dt][2 * j + 1], v_scale);
+      const bf16x8 vf = widen8(w[2 * j], w[2 * j + 1], v_scale);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) a.o[rt][dt] = mfma16(vf, pr[rt][j], a.o[rt][dt]);
     }
+  }
 }
 
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
+//
+// KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead.  KW = 1, many rows: bound by
+// the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers one block ahead (two buffers).
+template <int D, int RT, int KW> constexpr int kWavesPerSimd = D == 256 ? 1 : 2;
 template <int D, int RT, int KW, bool SPLIT>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares) {
+__global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares) {
   constexpr int RG = 4 / KW, M = 16 * RT * RG;
   __shared__ long long before[SPLIT ? kThreads + 1 : 1], wave_sums[4];
   __shared__ f32x4 joined[KW > 1 ? RG * KW / 2 * RT * (D / 16) * 64 : 1];
   __shared__ float joined_ml[KW > 1 ? 2 * 4 * RT * 16 : 1];
+  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? 2 * Staged<D>::kBytes : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int kw = wave % KW, rg = wave / KW;
@@ -303,6 +358,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_ker
     pos = share_begin(total, shares, w);
     end = share_begin(total, shares, w + 1);
     seg = locate(q, f, p.B, p.H_kv, pos);
+    if (tid == 0) reinterpret_cast<Join*>(p.partials)[w] = join_of(total, shares, w, seg);
   } else {
     seg.b = blockIdx.z;
     seg.h = blockIdx.x;
@@ -315,16 +371,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_ker
   }
 
   while (true) {
-    const int blk0 = (int)(pos - seg.begin), blk1 = (int)(min(end, seg.begin + seg.cost) - seg.begin);
-    const int blk_end = min(blk1, seg.blocks);
-    RowsOf<RT> rows;
-    find_rows(rows, p, seg.b, seg.t * M + rg * RT * 16, r);
-    int least = 0x7fffffff;
+    const int blk0 = uniform((int)(pos - seg.begin)), blk1 = uniform((int)(min(end, seg.begin + seg.cost) - seg.begin));
+    const int b = uniform(seg.b), h = uniform(seg.h), first_row = uniform(seg.t) * M + rg * RT * 16;
+    const int blk_end = min(blk1, uniform(seg.blocks));
+    int least = 0x7fffffff, limit[RT];
     bf16x8 qf[RT][D / 32];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      least = min(least, rows.limit[rt]);
-      const unsigned short* from = p.Q.at + seg.b * p.Q.sb + (seg.h * p.group + rows.head[rt]) * p.Q.sh + rows.query[rt] * p.Q.sn;
+      const Row x = find_row(p, b, first_row + rt * 16 + r);
+      limit[rt] = x.limit;
+      least = min(least, x.limit);
+      const unsigned short* from = p.Q.at + b * p.Q.sb + (h * p.group + x.head) * p.Q.sh + x.query * p.Q.sn;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) qf[rt][c] = *reinterpret_cast<const bf16x8*>(from + query_column<D>(c, g));
     }
@@ -334,23 +391,58 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_ker
 
     Acc<D, RT> a;
     a.clear();
-    const size_t bh = (size_t)seg.b * p.H_kv + seg.h;
-    const unsigned char* K = p.cache.K + bh * p.cache.capacity * D + key_offset(r, D);
-    const unsigned char* V = p.cache.V + bh * p.cache.capacity * D + r * kBlock + g * 16;
+    const size_t bh = (size_t)b * p.H_kv + h;
+    const unsigned char* K = p.cache.K + bh * p.cache.capacity * D;
+    const unsigned char* V = p.cache.V + bh * p.cache.capacity * D;
     const float* Ks = p.cache.K_scale + bh * nb;
     const float* Vs = p.cache.V_scale + bh * nb;
-    int blk = blk0 + kw;
-    KCodes<D> k;
-    if (blk < blk_end) k.load(K + (size_t)blk * (kBlock * D), g);
-    for (; blk < blk_end; blk += KW) {
-      u32x4 v[D / 16];
+    if constexpr (KW == 1) {
+      // a wave fetches every fourth piece; PIECES is a multiple of 4
+      constexpr int MINE = Staged<D>::PIECES / 4;
+      const unsigned buffers = uniform(lds_address(staged));
+      unsigned from[MINE];
 #pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt)
-        v[dt] = *reinterpret_cast<const u32x4*>(V + (size_t)blk * (kBlock * D) + dt * 16 * kBlock);
-      const float k_scale = Ks[blk], v_scale = Vs[blk];
-      block_step<D, RT>(a, qf, k, v, k_scale, v_scale, scale_log2, rows, blk * kBlock + kBlock > least, blk * kBlock, g, [&] {
-        if (blk + KW < blk_end) k.load(K + (size_t)(blk + KW) * (kBlock * D), g);
-      });
+      for (int i = 0; i < MINE; ++i) from[i] = Staged<D>::source(wave + 4 * i, lane);
+      auto fetch = [&](int blk, int buffer) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+          const int piece = wave + 4 * i;
+          fetch_piece((piece < Staged<D>::KP ? K : V) + (size_t)blk * (kBlock * D), from[i], buffers + buffer * Staged<D>::kBytes + piece * 1024);
+        }
+      };
+      const int at = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), at_odd = r * 32 + g * 8;
+      const bool rows_here = first_row < p.N * p.group;
+      __syncthreads();                                     // nobody reads the last segment's blocks any more
+      if (blk0 < blk_end) fetch(blk0, 0);
+      float k_scale = 0.f, v_scale = 0.f;
+      if (blk0 < blk_end) { k_scale = Ks[blk0]; v_scale = Vs[blk0]; }
+      for (int blk = blk0; blk < blk_end; ++blk) {
+        const int buffer = (blk - blk0) & 1;
+        wait_vmem();
+        __syncthreads();                                   // this block has landed, and the other buffer has been read
+        const float ks = k_scale, vs = v_scale;
+        if (blk + 1 < blk_end) {
+          fetch(blk + 1, buffer ^ 1);
+          k_scale = Ks[blk + 1];
+          v_scale = Vs[blk + 1];
+        }
+        if (!rows_here) continue;
+        const int base = (int)buffers + buffer * Staged<D>::kBytes;
+        const StagedBlock<D> codes{base + at, base + at_odd};
+        block_step<D, RT>(a, qf, codes, codes, ks, vs, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g, [] {});
+      }
+    } else {
+      const unsigned at = ((r >> 2) * 16 + (r & 3)) * D + g * 16, at_odd = ((r >> 2) * 16 + (r & 3)) * D + g * 8, at_v = r * kBlock + g * 16;
+      int blk = blk0 + kw;
+      KCodes<D> k;
+      if (blk < blk_end) k.load(K + (size_t)blk * (kBlock * D), at, at_odd);
+      for (; blk < blk_end; blk += KW) {
+        VCodes<D> v;
+        v.load(V + (size_t)blk * (kBlock * D), at_v);
+        block_step<D, RT>(a, qf, k, v, Ks[blk], Vs[blk], scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g, [&] {
+          if (blk + KW < blk_end) k.load(K + (size_t)(blk + KW) * (kBlock * D), at, at_odd);
+        });
+      }
     }
 
     a.join_groups();
@@ -394,9 +486,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_ker
     }
     if (kw == 0) {
       if (!SPLIT || (blk0 == 0 && blk1 == seg.cost)) {
-        store_rows<D, RT>(p, rows, seg.b, seg.h, a, g);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          store_row<D / 16>(p, find_row(p, b, first_row + rt * 16 + r), b, h, a.o[rt], a.m[rt], a.l[rt], 0, g);
       } else {
-        float* slot = p.partials + (size_t)(2 * w + (blk0 == 0 ? 1 : 0)) * kSlotFloats<D, RT, KW>;
+        float* slot = p.partials + most_shares * (sizeof(Join) / sizeof(float)) + (size_t)(2 * w + (blk0 == 0 ? 1 : 0)) * kSlotFloats<D, RT, KW>;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           const int tile = rg * RT + rt;
@@ -418,45 +512,59 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_ker
 }
 
 // Joins the parts of a segment that was split between shares: the work-group of the first share that begins inside it.  blockIdx.y is one row tile
-// of 16 and COLS / 16 of the D / 16 column tiles; the four waves take every fourth part and join theirs in LDS.
-template <int D, int RT, int KW, int DT>
-__global__ __launch_bounds__(kThreads) void attn_cache_merge_kernel(AttendArgs p, int tiles, int most_shares) {
-  constexpr int RG = 4 / KW, M = 16 * RT * RG, PARTS = D / 16 / DT;
-  __shared__ long long before[kThreads + 1], wave_sums[4];
-  __shared__ f32x4 joined[4][DT][64];
-  __shared__ float joined_ml[2][4][16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+// of 16 and DT of the D / 16 column tiles; the NW waves take every NW-th part, kAhead of them in flight, and join theirs in LDS.
+template <int D, int RT, int KW, int NW, int DT>
+__global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p, int shares_room) {
+  constexpr int RG = 4 / KW, M = 16 * RT * RG, PARTS = D / 16 / DT, kAhead = DT <= 2 ? 4 : 1;
+  __shared__ f32x4 joined[NW][DT][64];
+  __shared__ float joined_ml[2][NW][16];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int r = lane & 15, g = lane >> 4;
-  const Problem q{p.lengths, p.counts, p.cache.capacity, p.N, p.group, p.causal, tiles, M};
-  const Prefix f = make_prefix(q, p.B, before, wave_sums);
-  const long long total = p.H_kv * f(f.items);
-  const int shares = shares_of(total, most_shares, kLeastBlocks<KW>);
   const int w = blockIdx.x + 1;
-  if (w >= shares) return;
-  const long long begin = share_begin(total, shares, w);
-  const Segment seg = locate(q, f, p.B, p.H_kv, begin);
-  if (seg.begin == begin || share_begin(total, shares, w - 1) > seg.begin) return;
-  const long long seg_end = seg.begin + seg.cost;
+  const Join* notes = reinterpret_cast<const Join*>(p.partials);
+  if (w >= notes[0].parts) return;
+  const Join j = notes[w];
+  if (j.parts == 0) return;
+  const float* slots = p.partials + shares_room * (sizeof(Join) / sizeof(float));
   const int tile = blockIdx.y / PARTS, dt0 = (blockIdx.y % PARTS) * DT;
 
   f32x4 o[DT];
   float m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
-  for (int part = wave;; part += 4) {
-    const int share = w - 1 + part;
-    if (share >= shares || share_begin(total, shares, share) >= seg_end) break;
-    const float* slot = p.partials + (size_t)(2 * share + (part == 0 ? 1 : 0)) * kSlotFloats<D, RT, KW>;
-    const float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;
-    f32x4 x[DT];
+  for (int part = wave; part < j.parts; part += NW * kAhead) {
+    f32x4 x[kAhead][DT];
+    float mp[kAhead], lp[kAhead];
 #pragma unroll
-    for (int i = 0; i < DT; ++i) x[i] = reinterpret_cast<const f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + lane];
-    const float mp = ml[r], lp = ml[16 + r];
-    const float most = fmaxf(m, mp), use = most == -INFINITY ? 0.f : most;
-    const float mine = __builtin_amdgcn_exp2f(m - use), theirs = __builtin_amdgcn_exp2f(mp - use);
-    l = l * mine + lp * theirs;
+    for (int a = 0; a < kAhead; ++a) {
+      const bool there = part + a * NW < j.parts;
+      const float* slot = slots + (size_t)joined_slot(w, there ? part + a * NW : part) * kSlotFloats<D, RT, KW>;
+      const float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;
 #pragma unroll
-    for (int i = 0; i < DT; ++i) o[i] = o[i] * mine + x[i] * theirs;
+      for (int i = 0; i < DT; ++i) x[a][i] = reinterpret_cast<const f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + lane];
+      mp[a] = ml[r];
+      lp[a] = ml[16 + r];
+      if (!there) {                        // the same part again: it counts for nothing
+        mp[a] = -INFINITY;
+        lp[a] = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) x[a][i] = f32x4{0, 0, 0, 0};
+      }
+    }
+    float most = m;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) most = fmaxf(most, mp[a]);
+    const float use = most == -INFINITY ? 0.f : most, mine = __builtin_amdgcn_exp2f(m - use);
+    l *= mine;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] *= mine;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const float theirs = __builtin_amdgcn_exp2f(mp[a] - use);
+      l += lp[a] * theirs;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] += x[a][i] * theirs;
+    }
     m = most;
   }
   if (g == 0) { joined_ml[0][wave][r] = m; joined_ml[1][wave][r] = l; }
@@ -466,33 +574,19 @@ __global__ __launch_bounds__(kThreads) void attn_cache_merge_kernel(AttendArgs p
   if (wave != 0) return;
   float most = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) most = fmaxf(most, joined_ml[0][k][r]);
+  for (int k = 0; k < NW; ++k) most = fmaxf(most, joined_ml[0][k][r]);
   const float use = most == -INFINITY ? 0.f : most;
   l = 0.f;
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < NW; ++k) {
     const float by = __builtin_amdgcn_exp2f(joined_ml[0][k][r] - use);
     l += joined_ml[1][k][r] * by;
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] += joined[k][i][lane] * by;
   }
-  RowsOf<1> rows;
-  find_rows(rows, p, seg.b, seg.t * M + tile * 16, r);
-  if (rows.row[0] < 0) return;
-  const int head = seg.h * p.group + rows.head[0];
-  unsigned short* to = p.O + seg.b * p.o_sb + head * p.o_sh + rows.query[0] * p.o_sn;
-  const Divisor by = make_divisor(l);
-#pragma unroll
-  for (int i = 0; i < DT; ++i) {
-    union { bf16x4 v; uint2 w; } u;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) u.v[c] = rows.empty[0] ? (bf16_t)0.f : (bf16_t)divide(o[i][c], by);
-    *reinterpret_cast<uint2*>(to + (dt0 + i) * 16 + g * 4) = u.w;
-  }
-  if (dt0 == 0 && g == 0)
-    p.LSE[((size_t)seg.b * p.H + head) * p.N + rows.query[0]] = rows.empty[0] ? -INFINITY : (most + log2f(l)) * 0.6931471805599453f;
+  store_row<DT>(p, find_row(p, j.b, j.t * M + tile * 16 + r), j.b, j.h, o, most, l, dt0, g);
 }
 
 template <int D, int RT, int KW> hipError_t launch_fwd(const AttendArgs& p, const CacheForm& f, hipStream_t stream) {
@@ -502,15 +596,17 @@ template <int D, int RT, int KW> hipError_t launch_fwd(const AttendArgs& p, cons
   }
   attn_cache_fwd_kernel<D, RT, KW, true><<<(unsigned)((f.shares + 7) / 8 * 8), kThreads, 0, stream>>>(p, f.tiles, f.shares);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || f.shares == 1) return e;
-  constexpr int DT = KW == 4 ? 2 : D / 16;
-  attn_cache_merge_kernel<D, RT, KW, DT><<<dim3((unsigned)(f.shares - 1), (4 / KW) * RT * (D / 16 / DT)), kThreads, 0, stream>>>(p, f.tiles, f.shares);
+  const unsigned joins = (unsigned)(f.shares - 1), row_tiles = (4 / KW) * RT;
+  if (f.many_parts)
+    attn_cache_merge_kernel<D, RT, KW, 8, 2><<<dim3(joins, row_tiles * (D / 32)), 512, 0, stream>>>(p, f.shares);
+  else
+    attn_cache_merge_kernel<D, RT, KW, 2, D / 16><<<dim3(joins, row_tiles), 128, 0, stream>>>(p, f.shares);
   return hipGetLastError();
 }
 template <int D> hipError_t launch_fwd(const AttendArgs& p, hipStream_t stream) {
   const CacheForm f = cache_form(p.B, p.H, p.H_kv, p.N, D, p.cache.capacity);
   if (f.RT == 1) return launch_fwd<D, 1, 4>(p, f, stream);
   if (f.KW == 4) return launch_fwd<D, 2, 4>(p, f, stream);
-  if (f.KW == 2) return launch_fwd<D, 2, 2>(p, f, stream);
   return launch_fwd<D, 2, 1>(p, f, stream);
 }
 
@@ -534,13 +630,15 @@ template <int D, bool WG> __global__ __launch_bounds__(kThreads, 2) void attn_ca
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
   if (t0 < all && rows > 0) {
     KCodes<D> k;
-    k.load(p.cache.K + (bh * p.cache.capacity + t0) * D + key_offset(r, D), g);
+    const unsigned token = (r >> 2) * 16 + (r & 3);
+    k.load(p.cache.K + (bh * p.cache.capacity + t0) * D, token * D + g * 16, token * D + g * 8);
     const float k_scale = p.cache.K_scale[bh * nb + blk], scale_log2 = p.scale * kLog2e;
     bf16x8 kf[4][D / 32];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) kf[i][c] = k.frag(i, c, k_scale);
+      for (int c = 0; c < D / 32; ++c)
+        kf[i][c] = c < 2 * Cols<D>::C64 ? key_frag(k.whole(i, c / 2), c & 1, k_scale) : widen8(k.rest(i).x, k.rest(i).y, k_scale);
     // the first row that sees the block's first token
     const long long from = p.causal ? max(0ll, t0 - (length - n)) * p.group : 0;
     for (long long tile = from / 16 + (WG ? wave : 0); tile * 16 < rows; tile += WG ? 4 : 1) {
@@ -601,8 +699,7 @@ template <int D> hipError_t launch_weights(const WeighArgs& p, hipStream_t strea
 }  // namespace
 
 size_t attn_cache_fwd_partial_bytes(int B, int H, int H_kv, int N, int d, int capacity) {
-  const CacheForm f = cache_form(B, H, H_kv, N, d, capacity);
-  return f.split && f.shares > 1 ? 2 * (size_t)f.shares * f.slot_floats(d) * sizeof(float) : 0;
+  return cache_form(B, H, H_kv, N, d, capacity).workspace_bytes(d);
 }
 
 hipError_t attn_cache_fwd_dispatch(const AttendArgs& p, int d, hipStream_t stream) {

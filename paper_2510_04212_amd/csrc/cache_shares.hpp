@@ -4,7 +4,7 @@
 // `shares` work-groups take equal parts of all those blocks, wherever segments begin and end: sequences may differ in length
 // by any factor, and lengths are known on the device only.  A part of a segment is left in the workspace, in slot 2w + 1 of share w where
 // it begins the segment, 2w otherwise (a share ends inside one segment and begins inside one at most), and a second kernel
-// joins the parts.  A segment that sees nothing counts as one block, so that somebody writes its rows.
+// joins the parts: the first share that begins inside a segment leaves a note for it (Join).  A segment that sees nothing counts as one block, so that somebody writes its rows.
 //
 // Plain C++ (host and device).
 #pragma once
@@ -92,6 +92,18 @@ SHARES_FN int shares_of(long long total, int most, int least_blocks) {
   return s < 1 ? 1 : s > most ? most : (int)s;
 }
 SHARES_FN long long share_begin(long long total, int shares, int w) { return total * w / shares; }
+// What share w >= 1, which begins in s, notes for the joining kernel: parts of s, in shares w - 1 and the following; 0 where it is not the
+// first to begin inside s.  Note 0 holds the number of shares in `parts`.
+struct alignas(16) Join { int b, h, t, parts; };
+SHARES_FN Join join_of(long long total, int shares, int w, const Segment& s) {
+  Join j{s.b, s.h, s.t, 0};
+  if (w == 0) j.parts = shares;
+  else if (s.begin < share_begin(total, shares, w) && share_begin(total, shares, w - 1) <= s.begin)
+    j.parts = (int)(((s.begin + s.cost) * shares + total - 1) / total) - (w - 1);     // up to the first share that begins at its end or later
+  return j;
+}
+// Slot of part i of them.
+SHARES_FN int joined_slot(int w, int i) { return 2 * (w - 1 + i) + (i == 0 ? 1 : 0); }
 // Share of a work-group, or -1: neighbours in the list go to one XCD (work-groups are dealt to the eight in turn), as they read the
 // same head's cache.  The grid has a multiple of 8 work-groups, at least `shares`.
 SHARES_FN int share_of(int group, int shares) {
@@ -105,18 +117,22 @@ struct CacheForm {
   bool split;                              // shared out; otherwise a work-group per segment and nothing to join
   int rows() const { return 16 * RT * 4 / KW; }
   size_t slot_floats(int d) const { return (size_t)(4 / KW) * RT * (d / 16 * 256 + 32); }
+  bool many_parts;                         // few segments for the shares: each is in many parts
+  // notes, then slots
+  size_t workspace_bytes(int d) const { return split && shares > 1 ? shares * sizeof(Join) + 2 * (size_t)shares * slot_floats(d) * sizeof(float) : 0; }
 };
 template <int KW> constexpr int kLeastBlocks = KW == 4 ? 4 : 8;
 inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
   const long long rows = (long long)N * (H / H_kv);
   CacheForm f;
   f.RT = rows <= 16 ? 1 : 2;
-  f.KW = rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+  f.KW = rows <= 32 ? 4 : 1;
   f.tiles = (int)((rows + f.rows() - 1) / f.rows());
   const int nb = capacity / kBlock;
   f.split = nb > 16 || f.tiles > 65535;    // (the grid's second dimension)
   const double blocks = (double)B * H_kv * f.tiles * nb / (f.KW == 4 ? kLeastBlocks<4> : kLeastBlocks<1>);
   const int most = d == 256 ? 256 : 512;
   f.shares = blocks >= most ? most : blocks < 1 ? 1 : (int)blocks;
+  f.many_parts = f.shares > 4.0 * B * H_kv * f.tiles;
   return f;
 }

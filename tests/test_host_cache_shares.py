@@ -64,20 +64,17 @@ int main() {
       for (auto [from, to] : list) { if (from != at || to <= from) { printf("hole\n"); return 1; } at = to; }
       if (at != q.cost(std::get<0>(key), std::get<2>(key))) { printf("end missing\n"); return 1; }
     }
-    // the joining kernel's view: work-group w - 1 of shares - 1
+    // the joining kernel's view: the notes of shares 1 ..
     std::map<std::tuple<int, int, int>, int> joined;
-    for (int w = 1; w < shares; ++w) {
-      const long long begin = share_begin(total, shares, w);
-      const Segment s = locate(q, before, B, H, begin);
-      if (s.begin == begin || share_begin(total, shares, w - 1) > s.begin) continue;
-      const auto key = std::make_tuple(s.b, s.h, s.t);
+    for (int w = 0; w < shares; ++w) {
+      const Segment s = locate(q, before, B, H, share_begin(total, shares, w));
+      const Join j = join_of(total, shares, w, s);
+      if (w == 0 && j.parts != shares) { printf("first note\n"); return 1; }
+      if (w == 0 || j.parts == 0) continue;
+      const auto key = std::make_tuple(j.b, j.h, j.t);
       ++joined[key];
       std::vector<int> mine;
-      for (int part = 0;; ++part) {
-        const int share = w - 1 + part;
-        if (share >= shares || share_begin(total, shares, share) >= s.begin + s.cost) break;
-        mine.push_back(2 * share + (part == 0 ? 1 : 0));
-      }
+      for (int i = 0; i < j.parts; ++i) mine.push_back(joined_slot(w, i));
       if (mine != slots[key]) { printf("other parts joined\n"); return 1; }
     }
     for (auto& [key, list] : slots) if (joined[key] != 1) { printf("not joined once\n"); return 1; }
@@ -95,7 +92,7 @@ int main() {
   int B, H, Hkv, N, d, cap;
   while (scanf("%d %d %d %d %d %d", &B, &H, &Hkv, &N, &d, &cap) == 6) {
     const CacheForm f = cache_form(B, H, Hkv, N, d, cap);
-    printf("%d %d %d %d %d %zu\n", f.RT, f.KW, f.tiles, f.shares, (int)f.split, f.slot_floats(d));
+    printf("%d %d %d %d %d %zu %d\n", f.RT, f.KW, f.tiles, f.shares, (int)f.split, f.slot_floats(d), (int)f.many_parts);
   }
 }
 """
@@ -133,11 +130,12 @@ def test_the_form_covers_the_rows_and_the_workspace_is_what_the_library_says(tmp
     cases = [(B, Hkv * g, Hkv, N, d, cap) for B in (1, 3, 64) for Hkv in (1, 8) for g in (1, 4, 16) for N in (1, 2, 5, 16, 100, 2048)
              for cap in (64, 1024, 1088, 16384, 262144)]
     out = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in cases), check=True, capture_output=True, text=True).stdout
-    kinds = set()
+    kinds, many_parts = set(), set()
     for c, line in zip(cases, out.splitlines()):
-        RT, KW, tiles, shares, split, slot = map(int, line.split())
+        RT, KW, tiles, shares, split, slot, many = map(int, line.split())
         rows, M = c[3] * c[1] // c[2], 64 * RT // KW
         assert tiles * M >= rows > (tiles - 1) * M and 1 <= shares <= 512
-        assert binding.cache_fwd_workspace_bytes(*c) == (2 * shares * slot * 4 if split and shares > 1 else 0)
+        assert binding.cache_fwd_workspace_bytes(*c) == (16 * shares + 2 * shares * slot * 4 if split and shares > 1 else 0)
         kinds.add((RT, KW, bool(split)))
-    assert kinds == {(RT, KW, s) for RT, KW in ((1, 4), (2, 4), (2, 2), (2, 1)) for s in (False, True)}
+        many_parts.add((RT, KW, bool(many)))
+    assert kinds == many_parts == {(RT, KW, s) for RT, KW in ((1, 4), (2, 4), (2, 1)) for s in (False, True)}
