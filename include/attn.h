@@ -367,8 +367,9 @@ int attn_rope_frequencies(double* out, float* magnitude, int rot, double base, i
  * The cache of one layer, memory of the caller's with room for `capacity` tokens (a positive multiple of 64) of each sequence and head:
  *   K_cache  [B][H_kv][capacity][d]        8-bit codes, E4M3 (OCP 8-bit floating point; 0x7f and 0xff are NaN)
  *   V_cache  [B][H_kv][capacity/64][d][64] the same: a block of 64 tokens holds its columns one after the other
- *   K_scale, V_scale  float32 [B][H_kv][capacity/64]: a power of two for each block of 64 tokens of a head.
- * A code stands for its E4M3 value times its block's scale.  Memory need not be cleared: nothing behind a sequence's last
+ *   K_scale, V_scale  float32 [B][H_kv][capacity/64]: a power of two for each block of 64 tokens of a head; V's is negative where the
+ *                     block may hold NaN.
+ * A code stands for its E4M3 value times the magnitude of its block's scale.  Memory need not be cleared: nothing behind a sequence's last
  * token is interpreted.  B * H_kv * capacity * d < 2^40, capacity <= 2^30.
  */
 #define ATTN_CACHE_BLOCK 64
@@ -398,6 +399,8 @@ int attn_cache_append(const void* K, const void* V, const long long* strides, vo
  * A query that sees nothing, and queries i >= counts[b], give O = 0 and LSE = -infinity.  Scores, statistics and sums are float32, the row
  * sum that of the float32 probabilities; these are rounded to bf16 as the operand of the product with V, and O is rounded once.  A NaN among the values of a token does not reach the queries that do not see it.  Deterministic; which float32 sums
  * are formed in which order depends on the whole batch's lengths, as key blocks are shared out evenly over the chip.
+ * ATTN_ERR_UNSUPPORTED, for attn_cache_weights as well, where B * H_kv * T * (capacity / 64 + 5) >= 2^30 (seconds of work), T the number of
+ * tiles of 16, 32 or 128 that R = N H / H_kv rows make (R <= 16, <= 32, more).
  */
 size_t attn_cache_fwd_workspace_bytes(int B, int H, int H_kv, int N, int d, int capacity);
 int attn_cache_fwd(const void* Q, const long long* strides, const void* K_cache, const void* V_cache,

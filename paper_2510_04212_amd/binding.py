@@ -581,7 +581,7 @@ def attn_rope(Q, K=None, frequencies=None, positions=None, interleaved=False, ma
 
 class Cache(NamedTuple):
     """Keys and values of one layer in 8 bits (the layout is described in include/attn.h): K [B,H_kv,capacity,d] and V
-    [B,H_kv,capacity/64,d,64] in torch.float8_e4m3fn, K_scale and V_scale float32 [B,H_kv,capacity/64]."""
+    [B,H_kv,capacity/64,d,64] in torch.float8_e4m3fn, K_scale and V_scale float32 [B,H_kv,capacity/64] (V_scale negative: a NaN in the block)."""
     K: torch.Tensor
     V: torch.Tensor
     K_scale: torch.Tensor

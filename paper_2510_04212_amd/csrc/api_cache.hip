@@ -148,8 +148,10 @@ static int check_attend(int B, int H, int H_kv, int N, int d, int capacity, bool
   if (st != ATTN_OK || *empty) return st;
   if (H_kv < 1 || H < H_kv || H % H_kv != 0) return ATTN_ERR_BAD_ARG;
   if ((double)N * H >= 1073741824.0 || (double)B * N * H >= 274877906944.0) return ATTN_ERR_UNSUPPORTED;      // rows: counted in int per sequence
-  if ((double)B * ((double)N * (H / H_kv) / 16 + 1) >= 268435456.0) return ATTN_ERR_UNSUPPORTED;              // row tiles of the batch
-  return check_cache(B, H_kv, d, capacity);
+  const int st2 = check_cache(B, H_kv, d, capacity);
+  if (st2 != ATTN_OK) return st2;
+  // work of attn_cache_fwd is counted in int, in key blocks of row tiles (seconds of it, at this limit)
+  return cache_units(B, H_kv, cache_form(B, H, H_kv, N, d, capacity), capacity) < kUnitLimit ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
 }
 
 extern "C" size_t attn_cache_fwd_workspace_bytes(int B, int H, int H_kv, int N, int d, int capacity) {

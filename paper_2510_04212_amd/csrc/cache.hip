@@ -32,6 +32,12 @@ DEVI unsigned largest8(u32x4 x) {
   for (int j = 0; j < 4; ++j) m = max(m, max(magnitude(x[j] & 0xffffu), magnitude(x[j] >> 16)));
   return m;
 }
+DEVI unsigned any_nan8(u32x4 x) {
+  unsigned m = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m |= (unsigned)((x[j] & 0x7fffu) > 0x7f80u) | (unsigned)((x[j] & 0x7fffffffu) > 0x7f80ffffu);
+  return m;
+}
 DEVI float bf16_at(u32x4 x, int j) { return __uint_as_float((j & 1) ? x[j / 2] & 0xffff0000u : x[j / 2] << 16); }
 
 template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_append_kernel(AppendArgs p) {
@@ -54,7 +60,7 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_append_k
   auto is_new = [&](int t) { return index(t) >= 0 && index(t) < n; };
 
   u32x4 xk[NK], xv[NU][4];
-  unsigned mk = 0, mv = 0;
+  unsigned mk = 0, mv = 0, nan = 0;
 #pragma unroll
   for (int k = 0; k < NK; ++k) {
     const int v = tid + k * kThreads, t = v / CH, c = v % CH;
@@ -71,22 +77,27 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_append_k
     }
   }
   const int old_k = fresh ? kLowestExponent : exponent(p.cache.K_scale[at_scale]);
-  const int old_v = fresh ? kLowestExponent : exponent(p.cache.V_scale[at_scale]);
+  const float was_v = fresh ? power(kLowestExponent) : p.cache.V_scale[at_scale];
+  const int old_v = exponent(was_v);
 #pragma unroll
   for (int k = 0; k < NK; ++k) mk = max(mk, largest8(xk[k]));
 #pragma unroll
   for (int k = 0; k < NU; ++k)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) mv = max(mv, largest8(xv[k][j]));
-  __shared__ unsigned most[2][kThreads / 64];
+    for (int j = 0; j < 4; ++j) {
+      mv = max(mv, largest8(xv[k][j]));
+      nan |= any_nan8(xv[k][j]);
+    }
+  __shared__ unsigned most[2][kThreads / 64], nans[kThreads / 64];
   mk = max_over_wave(mk);
   mv = max_over_wave(mv);
-  if ((tid & 63) == 0) { most[0][tid >> 6] = mk; most[1][tid >> 6] = mv; }
+  nan = __any(nan != 0) ? 1u : 0u;
+  if ((tid & 63) == 0) { most[0][tid >> 6] = mk; most[1][tid >> 6] = mv; nans[tid >> 6] = nan; }
   __syncthreads();                                         // (every thread has read the old scales, too)
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) { mk = max(mk, most[0][w]); mv = max(mv, most[1][w]); }
+  for (int w = 0; w < kThreads / 64; ++w) { mk = max(mk, most[0][w]); mv = max(mv, most[1][w]); nan |= nans[w]; }
   const int ek = max(exponent_for(__uint_as_float(mk << 16)), old_k), ev = max(exponent_for(__uint_as_float(mv << 16)), old_v);
-  if (tid == 0) { p.cache.K_scale[at_scale] = power(ek); p.cache.V_scale[at_scale] = power(ev); }
+  if (tid == 0) { p.cache.K_scale[at_scale] = power(ek); p.cache.V_scale[at_scale] = nan || was_v < 0.f ? -power(ev) : power(ev); }
 
   // whole: every code of the block is written, zeros behind the last token; otherwise the new tokens' alone
   const bool whole_k = fresh || ek != old_k, whole_v = fresh || ev != old_v;
@@ -259,7 +270,9 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_gather_k
     if (p.weights_out)
       p.weights_out[bh * p.to.capacity + j * kBlock + tid] = real ? p.weights[bh * p.from.capacity + t] : 0.f;
     const size_t at = bh * (p.from.capacity / kBlock) + t / kBlock;
-    const int ek = real ? exponent(p.from.K_scale[at]) : -127, ev = real ? exponent(p.from.V_scale[at]) : -127;
+    const float vs = real ? p.from.V_scale[at] : 0.f;      // (its sign: NaN among the block's codes)
+    const int ek = real ? exponent(p.from.K_scale[at]) : -127, ev = real ? exponent(vs) : -127;
+    const bool nan = __any(vs < 0.f);
     const int mk = (int)max_over_wave((unsigned)(ek + 127)) - 127, mv = (int)max_over_wave((unsigned)(ev + 127)) - 127;
     source[tid] = t;
     times[0][tid] = power(max(ek - mk, -126));
@@ -270,7 +283,7 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_gather_k
       moved[1] = any_v;
       const size_t to = bh * (p.to.capacity / kBlock) + j;
       p.to.K_scale[to] = power(mk);
-      p.to.V_scale[to] = power(mv);
+      p.to.V_scale[to] = nan ? -power(mv) : power(mv);
     }
   }
   if (here <= 0) return;

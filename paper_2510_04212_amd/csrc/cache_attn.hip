@@ -51,8 +51,6 @@ template <int D> struct KCodes {
       if constexpr (Cols<D>::ODD) odd[i] = *reinterpret_cast<const u32x2*>(block + at_odd + (i * 4 * D + Cols<D>::C64 * 64));
     }
   }
-  DEVI u32x4 whole(int i, int k) const { return c[i][k]; }
-  DEVI u32x2 rest(int i) const { return odd[i]; }
 };
 template <int D> struct VCodes {
   u32x4 c[D / 16];
@@ -60,7 +58,6 @@ template <int D> struct VCodes {
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) c[dt] = *reinterpret_cast<const u32x4*>(block + at + dt * 1024);
   }
-  DEVI u32x4 operator()(int dt) const { return c[dt]; }
 };
 // From LDS, where a block's codes are shared by the four waves of a work-group.  Pieces of 1 KB, one transfer instruction each: 16 rows (tokens of
 // a tile, or columns of V) x 64 bytes, the four 16-byte chunks of row r permuted by slot_mask(r / 4) (common.hpp: 16 lanes reading
@@ -83,13 +80,20 @@ template <int D> struct Staged {
   }
 };
 typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
-typedef __attribute__((address_space(3))) const u32x2 lds_uint2;
-template <int D> struct StagedBlock {
-  int at, at_odd;                       // LDS addresses: the buffer's + the lane's
-  DEVI u32x4 whole(int i, int k) const { return *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (i * Cols<D>::C64 + k) * 1024)); }
-  DEVI u32x2 rest(int i) const { return *reinterpret_cast<lds_uint2*>((unsigned long)(unsigned)(at_odd + 4 * Cols<D>::C64 * 1024 + i * 512)); }
-  DEVI u32x4 operator()(int dt) const { return *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (Staged<D>::KP + dt) * 1024)); }
-};
+typedef __attribute__((address_space(3))) const u32x2 lds_u32x2;
+// at, at_odd: LDS addresses, the buffer's + the lane's
+template <int D> DEVI void read_staged(KCodes<D>& k, int at, int at_odd) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int c = 0; c < Cols<D>::C64; ++c) k.c[i][c] = *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (i * Cols<D>::C64 + c) * 1024));
+    if constexpr (Cols<D>::ODD) k.odd[i] = *reinterpret_cast<lds_u32x2*>((unsigned long)(unsigned)(at_odd + 4 * Cols<D>::C64 * 1024 + i * 512));
+  }
+}
+template <int D> DEVI void read_staged(VCodes<D>& v, int at) {
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) v.c[dt] = *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (Staged<D>::KP + dt) * 1024));
+}
 // 64 lanes' 16 bytes each from block + at into LDS at `to` .. + 1023; `block` and `to` the same in all lanes.  Inline assembly as in common.hpp's
 // TileLoader, and for its reasons; waited for with wait_vmem().
 DEVI void fetch_piece(const unsigned char* block, unsigned at, unsigned to) {
@@ -110,39 +114,58 @@ DEVI float max_over_groups(float x) {
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 DEVI int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-DEVI long long uniform(long long x) {
-  return (long long)(((unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32) | (unsigned)uniform((int)x));
-}
 
-// ---- The list of key blocks (cache_shares.hpp): sums of cost over runs of (sequence, tile) items, in LDS; before[k]: items 0 .. k run - 1.
-struct Prefix {
-  const Problem& q;
-  int items, run;
-  const long long* before;
-  DEVI long long operator()(int item) const {
-    const int k = item / run;
-    long long s = before[k];
-    for (int i = k * run; i < item; ++i) s += q.cost(i / q.tiles, i % q.tiles);
-    return uniform(s);
-  }
+// ---- The list of segments (cache_shares.hpp): every thread sums up the units of a run of (sequence, tile) items, for one head; a scan over the threads.
+struct Runs {
+  int before[kThreads + 1];                // units in front of thread t's run
+  int waves[kThreads / 64];
+  Segment segment;
 };
-DEVI Prefix make_prefix(const Problem& q, int B, long long* before, long long* waves) {
-  const int items = B * q.tiles, run = (items + kThreads - 1) / kThreads;
+// units of all items
+DEVI int scan_units(const Problem& q, int items, int run, Runs& runs) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  long long x = 0;
+  int x = 0;
   for (int i = tid * run; i < min(items, (tid + 1) * run); ++i) x += q.cost(i / q.tiles, i % q.tiles);
 #pragma unroll
   for (int i = 1; i < 64; i <<= 1) {
-    const long long y = __shfl_up(x, i);
+    const int y = __shfl_up(x, i);
     if (lane >= i) x += y;
   }
-  if (lane == 63) waves[wave] = x;
+  if (lane == 63) runs.waves[wave] = x;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) x += waves[w];
-  before[tid + 1] = x;
-  if (tid == 0) before[0] = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64 - 1; ++w) x += w < wave ? runs.waves[w] : 0;
+  runs.before[tid + 1] = x;
+  if (tid == 0) runs.before[0] = 0;
   __syncthreads();
-  return Prefix{q, items, run, before};
+  return uniform(runs.before[kThreads]);
+}
+// The segment of unit `pos`, found by the thread whose run holds it.
+DEVI Segment find_segment(const Problem& q, int B, int H_kv, int run, int pos, Runs& runs) {
+  auto units_before = [&](int item) {      // in front of an item
+    int x = runs.before[item / run];
+    for (int i = item / run * run; i < item; ++i) x += q.cost(i / q.tiles, i % q.tiles);
+    return x;
+  };
+  const int tid = threadIdx.x;
+  int b = -1, first = 0, each = 0, here = runs.before[tid];
+  for (int i = tid * run; i < min(B * q.tiles, (tid + 1) * run); ++i) {
+    if (i / q.tiles != b) {
+      b = i / q.tiles;
+      first = units_before(b * q.tiles);
+      each = units_before((b + 1) * q.tiles) - first;
+    }
+    Segment s;
+    if (locate(q, b, i % q.tiles, first, each, here - first, H_kv, pos, &s)) runs.segment = s;
+    here += q.cost(b, i % q.tiles);
+  }
+  __syncthreads();
+  Segment s = runs.segment;
+  s.b = uniform(s.b);
+  s.h = uniform(s.h);
+  s.t = uniform(s.t);
+  s.begin = uniform(s.begin);
+  return s;
 }
 
 // ---- state of a wave's rows: lane (r, g) has row r of each of its RT tiles, output columns 16 dt + 4 g .. + 3
@@ -206,45 +229,43 @@ DEVI void store_row(const AttendArgs& p, const Row& x, int b, int h, const f32x4
   if (dt0 == 0 && g == 0) p.LSE[((size_t)b * p.H + head) * p.N + x.query] = x.empty ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// every load but the n youngest has landed (s_waitcnt vmcnt(n))
+template <int n> DEVI void wait_vmem_but() { __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14); }
+
 // bytes of w that are 0x7f or 0xff, E4M3's NaN: 0x80 in each of them
 DEVI unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-DEVI u32x4 without_nan(u32x4 w) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] &= ~((nan_codes(w[i]) >> 7) * 0xffu);
-  return w;
-}
-
-// A masked block: does its V hold NaN?  0 * NaN must not reach the rows that do not see that token, so its codes count as 0 then, and an
+// A masked block whose V holds NaN: 0 * NaN must not reach the rows that do not see that token.  The codes are made 0, and an
 // output to which a row's visible tokens bring a NaN is made one: that count is a product, too, of ones.
-template <int D, int RT, class V>
-DEVI bool take_out_nan(Acc<D, RT>& a, const V& v, const int (&limit)[RT], int t0, int g) {
-  bool any = false;
+template <int D, int RT>
+DEVI void take_out_nan(Acc<D, RT>& a, VCodes<D>& v, const int (&limit)[RT], int t0, int g) {
+  int seen[RT];
 #pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) {
-    const u32x4 w = v(dt);
-    const unsigned bad = nan_codes(w[0]) | nan_codes(w[1]) | nan_codes(w[2]) | nan_codes(w[3]);
-    if (!__any(bad != 0)) continue;
-    any = true;
+  for (int rt = 0; rt < RT; ++rt) {
+    seen[rt] = limit[rt] - t0 - 16 * g;
+    settle(seen[rt]);                      // (a copy: or the masks are formed for both uses at once, and kept)
+  }
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const unsigned lo = nan_codes(w[2 * j]), hi = nan_codes(w[2 * j + 1]);
+      const unsigned lo = nan_codes(v.c[dt][2 * j]), hi = nan_codes(v.c[dt][2 * j + 1]);
+      v.c[dt][2 * j] &= ~((lo >> 7) * 0xffu);
+      v.c[dt][2 * j + 1] &= ~((hi >> 7) * 0xffu);
       bf16x8 ones;
 #pragma unroll
       for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)((((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0x80u) ? 1.f : 0.f);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        bf16x8 seen;
+        bf16x8 sees;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) seen[e] = (bf16_t)(t0 + 16 * g + 8 * j + e < limit[rt] ? 1.f : 0.f);
-        const f32x4 count = mfma16(ones, seen, f32x4{0, 0, 0, 0});
+        for (int e = 0; e < 8; ++e) sees[e] = (bf16_t)(8 * j + e < seen[rt] ? 1.f : 0.f);
+        const f32x4 count = mfma16(ones, sees, f32x4{0, 0, 0, 0});
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (count[i] > 0.f) a.o[rt][dt][i] = NAN;
       }
     }
-  }
-  return any;
 }
 
 // One block of 64 tokens for a wave's rows.  masked (the same in all lanes): some row does not see all of it.  after_scores() is called when
@@ -253,8 +274,8 @@ DEVI bool take_out_nan(Acc<D, RT>& a, const V& v, const int (&limit)[RT], int t0
 // The maximum that probabilities are taken relative to is let fall behind the true one by up to kSlack (a factor of 2^kSlack, harmless in float32 and
 // bf16 alike), so that the accumulators are hardly ever rescaled.
 constexpr float kSlack = 8.f;
-template <int D, int RT, class K, class V, class F>
-DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, const V& v, float k_scale, float v_scale, float scale_log2,
+template <int D, int RT, class F>
+DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, float scale_log2,
                      const int (&limit)[RT], bool masked, int t0, int g, F&& after_scores) {
   f32x4 s[RT][4];
 #pragma unroll
@@ -265,7 +286,7 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, c
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int c = 0; c < Cols<D>::C64; ++c) {
-      const u32x4 w = k.whole(i, c);
+      const u32x4 w = k.c[i][c];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const bf16x8 kf = key_frag(w, half, k_scale);
@@ -274,14 +295,13 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, c
       }
     }
     if constexpr (Cols<D>::ODD) {
-      const u32x2 w = k.rest(i);
+      const u32x2 w = k.odd[i];
       const bf16x8 kf = widen8(w.x, w.y, k_scale);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][D / 32 - 1], s[rt][i]);
     }
   }
   after_scores();
-  bool nan = false;
   if (masked) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -290,8 +310,9 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, c
       for (int i = 0; i < 16; ++i)
         if (i >= seen) s[rt][i / 4][i % 4] = -INFINITY;
     }
-    nan = take_out_nan<D, RT>(a, v, limit, t0, g);
+    if (v_scale < 0.f) take_out_nan<D, RT>(a, v, limit, t0, g);          // V's scale is negative: a code of the block is NaN
   }
+  v_scale = __builtin_fabsf(v_scale);
   bf16x8 pr[RT][2];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -316,8 +337,7 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, c
   }
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
-    u32x4 w = v(dt);
-    if (nan) w = without_nan(w);
+    const u32x4 w = v.c[dt];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const bf16x8 vf = widen8(w[2 * j], w[2 * j + 1], v_scale);
@@ -330,15 +350,17 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const K& k, c
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
 //
 // KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead.  KW = 1, many rows: bound by
-// the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers one block ahead (two buffers).
+// the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers kBuffers - 1 blocks ahead.
+constexpr int kBuffers = 4;
 template <int D, int RT, int KW> constexpr int kWavesPerSimd = D == 256 ? 1 : 2;
 template <int D, int RT, int KW, bool SPLIT>
 __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares) {
   constexpr int RG = 4 / KW, M = 16 * RT * RG;
-  __shared__ long long before[SPLIT ? kThreads + 1 : 1], wave_sums[4];
-  __shared__ f32x4 joined[KW > 1 ? RG * KW / 2 * RT * (D / 16) * 64 : 1];
-  __shared__ float joined_ml[KW > 1 ? 2 * 4 * RT * 16 : 1];
-  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? 2 * Staged<D>::kBytes : 16];
+  static_assert(KW == 1 || KW == 4, "the four waves have rows of their own, or blocks");
+  __shared__ Runs runs;
+  __shared__ f32x4 joined[KW == 4 ? 4 * RT * (D / 16) * 64 : 1];         // [wave][RT][D / 16][lane]
+  __shared__ float joined_m[KW == 4 ? 4 * RT * 16 : 1], joined_l[KW == 4 ? 4 * RT * 16 : 1];
+  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? kBuffers * Staged<D>::kBytes : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int kw = wave % KW, rg = wave / KW;
@@ -347,33 +369,47 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
   const float scale_log2 = p.scale * kLog2e;
 
   Segment seg;
-  long long pos, end;
-  int w = 0;
+  int pos, end, w = 0;
   if constexpr (SPLIT) {
-    const Prefix f = make_prefix(q, p.B, before, wave_sums);
-    const long long total = p.H_kv * f(f.items);
-    const int shares = shares_of(total, most_shares, kLeastBlocks<KW>);
-    w = share_of(blockIdx.x, shares);
+    const int items = p.B * tiles, run = (items + kThreads - 1) / kThreads;
+    const Shares all = shares_of(p.H_kv * scan_units(q, items, run, runs), most_shares, kLeastUnits<KW>);
+    w = share_of(blockIdx.x, all.number);
     if (w < 0) return;
-    pos = share_begin(total, shares, w);
-    end = share_begin(total, shares, w + 1);
-    seg = locate(q, f, p.B, p.H_kv, pos);
-    if (tid == 0) reinterpret_cast<Join*>(p.partials)[w] = join_of(total, shares, w, seg);
+    pos = uniform(all.begin(w));
+    end = uniform(all.begin(w + 1));
+    seg = find_segment(q, p.B, p.H_kv, run, pos, runs);
+    if (tid == 0) reinterpret_cast<Join*>(p.partials)[w] = join_of(all, w, seg);
   } else {
     seg.b = blockIdx.z;
     seg.h = blockIdx.x;
     seg.t = blockIdx.y;
     seg.begin = 0;
     seg.blocks = q.blocks(seg.b, seg.t);
-    seg.cost = max(1, seg.blocks);
     pos = 0;
-    end = seg.cost;
+    end = seg.end();
   }
+  seg.blocks = uniform(seg.blocks);
 
   while (true) {
-    const int blk0 = uniform((int)(pos - seg.begin)), blk1 = uniform((int)(min(end, seg.begin + seg.cost) - seg.begin));
-    const int b = uniform(seg.b), h = uniform(seg.h), first_row = uniform(seg.t) * M + rg * RT * 16;
-    const int blk_end = min(blk1, uniform(seg.blocks));
+    const int to = min(end, seg.end());
+    const int b = seg.b, h = seg.h, first_row = seg.t * M + rg * RT * 16;
+    const int blk0 = seg.block_at(pos), blk_end = seg.block_at(to);
+    const size_t bh = (size_t)b * p.H_kv + h;
+    const unsigned char* K = p.cache.K + bh * p.cache.capacity * D;
+    const unsigned char* V = p.cache.V + bh * p.cache.capacity * D;
+    const float* Ks = p.cache.K_scale + bh * nb;
+    const float* Vs = p.cache.V_scale + bh * nb;
+    // a wave of few rows: its first block is on its way while the queries are looked for
+    const unsigned at = ((r >> 2) * 16 + (r & 3)) * D + g * 16, at_odd = ((r >> 2) * 16 + (r & 3)) * D + g * 8, at_v = r * kBlock + g * 16;
+    KCodes<D> k;
+    float k_scale = 0.f, next_v = 0.f;     // loaded with K's codes: a load behind V's would have V waited for
+    auto load_key = [&](int blk) {
+      if (blk >= blk_end) return;
+      k_scale = Ks[blk];
+      next_v = Vs[blk];
+      k.load(K + (size_t)blk * (kBlock * D), at, at_odd);
+    };
+    if constexpr (KW == 4) load_key(blk0 + kw);
     int least = 0x7fffffff, limit[RT];
     bf16x8 qf[RT][D / 32];
 #pragma unroll
@@ -391,11 +427,6 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
 
     Acc<D, RT> a;
     a.clear();
-    const size_t bh = (size_t)b * p.H_kv + h;
-    const unsigned char* K = p.cache.K + bh * p.cache.capacity * D;
-    const unsigned char* V = p.cache.V + bh * p.cache.capacity * D;
-    const float* Ks = p.cache.K_scale + bh * nb;
-    const float* Vs = p.cache.V_scale + bh * nb;
     if constexpr (KW == 1) {
       // a wave fetches every fourth piece; PIECES is a multiple of 4
       constexpr int MINE = Staged<D>::PIECES / 4;
@@ -410,104 +441,125 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
           fetch_piece((piece < Staged<D>::KP ? K : V) + (size_t)blk * (kBlock * D), from[i], buffers + buffer * Staged<D>::kBytes + piece * 1024);
         }
       };
-      const int at = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), at_odd = r * 32 + g * 8;
+      const int in_piece = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), in_odd = r * 32 + g * 8;
       const bool rows_here = first_row < p.N * p.group;
+      // Scales: 64 blocks' at a time, one in each lane.
+      float k_scales = 0.f, v_scales = 0.f;
+      auto load_scales = [&](int blk) {
+        const int mine = min(blk + lane, nb - 1);
+        k_scales = Ks[mine];
+        v_scales = Vs[mine];
+        settle(k_scales);
+        settle(v_scales);
+      };
       __syncthreads();                                     // nobody reads the last segment's blocks any more
-      if (blk0 < blk_end) fetch(blk0, 0);
-      float k_scale = 0.f, v_scale = 0.f;
-      if (blk0 < blk_end) { k_scale = Ks[blk0]; v_scale = Vs[blk0]; }
+      if (blk0 < blk_end) {
+        fetch(blk0, 0);
+        load_scales(blk0);
+      }
+      // What the compiler has loaded is settled here: waits that it placed inside the loop, where it knows nothing of the transfers, would wait for these.
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) settle(qf[rt][c]);
+#pragma unroll
+      for (int i = 1; i < kBuffers - 1; ++i)
+        if (blk0 + i < blk_end) fetch(blk0 + i, i);
+      int buffer = 0;
       for (int blk = blk0; blk < blk_end; ++blk) {
-        const int buffer = (blk - blk0) & 1;
-        wait_vmem();
-        __syncthreads();                                   // this block has landed, and the other buffer has been read
-        const float ks = k_scale, vs = v_scale;
-        if (blk + 1 < blk_end) {
-          fetch(blk + 1, buffer ^ 1);
-          k_scale = Ks[blk + 1];
-          v_scale = Vs[blk + 1];
+        static_assert(kBuffers == 4, "transfers behind this block's: two blocks' at most");
+        const int behind = blk_end - 1 - blk;
+        if (behind >= 2) wait_vmem_but<2 * MINE>();
+        else if (behind == 1) wait_vmem_but<MINE>();
+        else wait_vmem();
+        __syncthreads();                                   // this block has landed for all waves, and all have read the one before
+        if (behind >= kBuffers - 1) fetch(blk + kBuffers - 1, (buffer + kBuffers - 1) % kBuffers);
+        if (rows_here) {
+          if (blk > blk0 && ((blk - blk0) & 63) == 0) load_scales(blk);
+          const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), (blk - blk0) & 63));
+          const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), (blk - blk0) & 63));
+          const int base = (int)buffers + buffer * Staged<D>::kBytes;
+          VCodes<D> v;
+          read_staged<D>(k, base + in_piece, base + in_odd);
+          block_step<D, RT>(a, qf, k, v, ks, vs, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g,
+                            [&] { read_staged<D>(v, base + in_piece); });
         }
-        if (!rows_here) continue;
-        const int base = (int)buffers + buffer * Staged<D>::kBytes;
-        const StagedBlock<D> codes{base + at, base + at_odd};
-        block_step<D, RT>(a, qf, codes, codes, ks, vs, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g, [] {});
+        buffer = (buffer + 1) % kBuffers;
       }
     } else {
-      const unsigned at = ((r >> 2) * 16 + (r & 3)) * D + g * 16, at_odd = ((r >> 2) * 16 + (r & 3)) * D + g * 8, at_v = r * kBlock + g * 16;
-      int blk = blk0 + kw;
-      KCodes<D> k;
-      if (blk < blk_end) k.load(K + (size_t)blk * (kBlock * D), at, at_odd);
-      for (; blk < blk_end; blk += KW) {
+      for (int blk = blk0 + kw; blk < blk_end; blk += KW) {
         VCodes<D> v;
         v.load(V + (size_t)blk * (kBlock * D), at_v);
-        block_step<D, RT>(a, qf, k, v, Ks[blk], Vs[blk], scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g, [&] {
-          if (blk + KW < blk_end) k.load(K + (size_t)(blk + KW) * (kBlock * D), at, at_odd);
-        });
+        block_step<D, RT>(a, qf, k, v, k_scale, next_v, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g,
+                          [&] { load_key(blk + KW); });
       }
     }
 
     a.join_groups();
-    // the KW waves of a row group: one maximum, then two halves at a time
-    if constexpr (KW > 1) {
-      if (g == 0)
+    const bool whole = !SPLIT || (pos == seg.begin && to == seg.end());
+    float* slot = p.partials + most_shares * (sizeof(Join) / sizeof(float)) + (size_t)(2 * w + (pos == seg.begin ? 1 : 0)) * kSlotFloats<D, RT, KW>;
+    // O and LSE of a finished row, or this part of them: column tiles dt0 .. dt0 + DT - 1 of row tile `tile`
+    auto put = [&](auto DT, int tile, const f32x4* o, float m, float l, int dt0) {
+      if (whole) {
+        store_row<DT>(p, find_row(p, b, seg.t * M + tile * 16 + r), b, h, o, m, l, dt0, g);
+        return;
+      }
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) joined_ml[(wave * RT + rt) * 16 + r] = a.m[rt];
-      __syncthreads();
+      for (int i = 0; i < DT; ++i) reinterpret_cast<f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + lane] = o[i];
+      float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;
+      if (g == 0 && dt0 == 0) {
+        ml[r] = m;
+        ml[16 + r] = l;
+      }
+    };
+    if constexpr (KW == 1) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) put(std::integral_constant<int, D / 16>{}, rg * RT + rt, a.o[rt], a.m[rt], a.l[rt], 0);
+    } else {
+      // Four waves have four sums of the same rows: all go to LDS as they are, and each wave joins RT * D / 64 of the RT * D / 16 tiles
+      // (d = 32: the first two).
+      __syncthreads();                                     // the last segment's have been read
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        float m = -INFINITY;
 #pragma unroll
-        for (int o = 0; o < KW; ++o) m = fmaxf(m, joined_ml[((rg * KW + o) * RT + rt) * 16 + r]);
-        a.scale(rt, __builtin_amdgcn_exp2f(a.m[rt] - (m == -INFINITY ? 0.f : m)));
-        a.m[rt] = m;
+        for (int dt = 0; dt < D / 16; ++dt) joined[((wave * RT + rt) * (D / 16) + dt) * 64 + lane] = a.o[rt][dt];
+        if (g == 0) {
+          joined_m[(wave * RT + rt) * 16 + r] = a.m[rt];
+          joined_l[(wave * RT + rt) * 16 + r] = a.l[rt];
+        }
       }
-      float* joined_l = joined_ml + 4 * RT * 16;
+      __syncthreads();
+      constexpr int EACH = D / 16 >= 4 ? D / 16 / 4 : 1, REST = D / 16 - 4 * EACH;       // column tiles per wave (d = 96: 1, and 2 that are left)
 #pragma unroll
-      for (int half = KW / 2; half >= 1; half /= 2) {
-        f32x4* mine = joined + (rg * (KW / 2) + (kw & (half - 1))) * RT * (D / 16) * 64 + lane;
-        if (kw >= half && kw < 2 * half) {
+      for (int rt = 0; rt < RT; ++rt) {
+        float by[4], m = -INFINITY, l = 0.f;
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
+        for (int x = 0; x < 4; ++x) m = fmaxf(m, joined_m[(x * RT + rt) * 16 + r]);
+        const float use = m == -INFINITY ? 0.f : m;
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) mine[(rt * (D / 16) + dt) * 64] = a.o[rt][dt];
-            if (g == 0) joined_l[(wave * RT + rt) * 16 + r] = a.l[rt];
-          }
+        for (int x = 0; x < 4; ++x) {
+          by[x] = __builtin_amdgcn_exp2f(joined_m[(x * RT + rt) * 16 + r] - use);
+          l += joined_l[(x * RT + rt) * 16 + r] * by[x];
         }
-        __syncthreads();
-        if (kw < half) {
+        auto join = [&](auto DT, int dt0) {
+          f32x4 o[DT];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
+          for (int i = 0; i < DT; ++i) {
+            o[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) a.o[rt][dt] += mine[(rt * (D / 16) + dt) * 64];
-            a.l[rt] += joined_l[((wave + half) * RT + rt) * 16 + r];
+            for (int x = 0; x < 4; ++x) o[i] += joined[((x * RT + rt) * (D / 16) + dt0 + i) * 64 + lane] * by[x];
           }
-        }
-        __syncthreads();
-      }
-    }
-    if (kw == 0) {
-      if (!SPLIT || (blk0 == 0 && blk1 == seg.cost)) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          store_row<D / 16>(p, find_row(p, b, first_row + rt * 16 + r), b, h, a.o[rt], a.m[rt], a.l[rt], 0, g);
-      } else {
-        float* slot = p.partials + most_shares * (sizeof(Join) / sizeof(float)) + (size_t)(2 * w + (blk0 == 0 ? 1 : 0)) * kSlotFloats<D, RT, KW>;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const int tile = rg * RT + rt;
-#pragma unroll
-          for (int dt = 0; dt < D / 16; ++dt) reinterpret_cast<f32x4*>(slot)[(tile * (D / 16) + dt) * 64 + lane] = a.o[rt][dt];
-          float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;
-          if (g == 0) {
-            ml[r] = a.m[rt];
-            ml[16 + r] = a.l[rt];
-          }
-        }
+          put(DT, rt, o, m, l, dt0);
+        };
+        if (wave * EACH < D / 16) join(std::integral_constant<int, EACH>{}, wave * EACH);
+        if (REST > 0 && wave < REST) join(std::integral_constant<int, 1>{}, 4 * EACH + wave);
       }
     }
     if constexpr (!SPLIT) break;
-    pos = seg.begin + blk1;
+    pos = to;
     if (pos >= end) break;
     next_segment(q, p.H_kv, seg);
+    seg.blocks = uniform(seg.blocks);
   }
 }
 
@@ -522,9 +574,9 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p,
   const int r = lane & 15, g = lane >> 4;
   const int w = blockIdx.x + 1;
   const Join* notes = reinterpret_cast<const Join*>(p.partials);
-  if (w >= notes[0].parts) return;
-  const Join j = notes[w];
-  if (j.parts == 0) return;
+  const int shares = notes[0].parts;
+  const Join j = notes[w];                 // there is room for it, whether there is such a share or not
+  if (w >= shares || j.parts == 0) return;
   const float* slots = p.partials + shares_room * (sizeof(Join) / sizeof(float));
   const int tile = blockIdx.y / PARTS, dt0 = (blockIdx.y % PARTS) * DT;
 
@@ -579,7 +631,7 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p,
   l = 0.f;
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
+#pragma unroll 4
   for (int k = 0; k < NW; ++k) {
     const float by = __builtin_amdgcn_exp2f(joined_ml[0][k][r] - use);
     l += joined_ml[1][k][r] * by;
@@ -598,15 +650,15 @@ template <int D, int RT, int KW> hipError_t launch_fwd(const AttendArgs& p, cons
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || f.shares == 1) return e;
   const unsigned joins = (unsigned)(f.shares - 1), row_tiles = (4 / KW) * RT;
   if (f.many_parts)
-    attn_cache_merge_kernel<D, RT, KW, 8, 2><<<dim3(joins, row_tiles * (D / 32)), 512, 0, stream>>>(p, f.shares);
+    attn_cache_merge_kernel<D, RT, KW, 16, 2><<<dim3(joins, row_tiles * (D / 32)), 1024, 0, stream>>>(p, f.shares);
   else
     attn_cache_merge_kernel<D, RT, KW, 2, D / 16><<<dim3(joins, row_tiles), 128, 0, stream>>>(p, f.shares);
   return hipGetLastError();
 }
 template <int D> hipError_t launch_fwd(const AttendArgs& p, hipStream_t stream) {
   const CacheForm f = cache_form(p.B, p.H, p.H_kv, p.N, D, p.cache.capacity);
-  if (f.RT == 1) return launch_fwd<D, 1, 4>(p, f, stream);
-  if (f.KW == 4) return launch_fwd<D, 2, 4>(p, f, stream);
+  if (f.KW == 4) return launch_fwd<D, 1, 4>(p, f, stream);
+  if (f.RT == 1) return launch_fwd<D, 1, 1>(p, f, stream);
   return launch_fwd<D, 2, 1>(p, f, stream);
 }
 
@@ -638,7 +690,7 @@ template <int D, bool WG> __global__ __launch_bounds__(kThreads, 2) void attn_ca
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int c = 0; c < D / 32; ++c)
-        kf[i][c] = c < 2 * Cols<D>::C64 ? key_frag(k.whole(i, c / 2), c & 1, k_scale) : widen8(k.rest(i).x, k.rest(i).y, k_scale);
+        kf[i][c] = c < 2 * Cols<D>::C64 ? key_frag(k.c[i][c / 2], c & 1, k_scale) : widen8(k.odd[i].x, k.odd[i].y, k_scale);
     // the first row that sees the block's first token
     const long long from = p.causal ? max(0ll, t0 - (length - n)) * p.group : 0;
     for (long long tile = from / 16 + (WG ? wave : 0); tile * 16 < rows; tile += WG ? 4 : 1) {

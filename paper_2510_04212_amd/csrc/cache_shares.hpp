@@ -1,10 +1,10 @@
 // How the work of an attn_cache_fwd call is shared out, and which form of its kernels serves it.
 //
-// A call is a list of segments (sequence, key/value head, tile of query rows), in this order, of so many key blocks each, and
-// `shares` work-groups take equal parts of all those blocks, wherever segments begin and end: sequences may differ in length
-// by any factor, and lengths are known on the device only.  A part of a segment is left in the workspace, in slot 2w + 1 of share w where
-// it begins the segment, 2w otherwise (a share ends inside one segment and begins inside one at most), and a second kernel
-// joins the parts: the first share that begins inside a segment leaves a note for it (Join).  A segment that sees nothing counts as one block, so that somebody writes its rows.
+// A call is a list of segments (sequence, key/value head, tile of query rows), in this order, of so many units of work each: kStart to
+// begin and end one, then one for each of its key blocks.  `shares` work-groups take equal parts of all units, wherever segments begin and
+// end: sequences may differ in length by any factor, and lengths are known on the device only.  A part of a segment is left in the
+// workspace, in slot 2w + 1 of share w where it begins the segment, 2w otherwise (a share ends inside one segment and begins inside one at
+// most), and a second kernel joins the parts: the first share that begins inside a segment leaves a note for it (Join).
 //
 // Plain C++ (host and device).
 #pragma once
@@ -16,6 +16,10 @@
 #define SHARES_FN inline
 #endif
 
+// Reading the queries, filling the pipeline, joining the waves and storing takes a work-group about as long as kStart key blocks: without
+// it, the shares of short sequences take longer than the others (one token of 64 sequences of 64 to 8192 tokens, H 32/8, d 128: 160 us
+// at 0, 139 at 1, 121 at 3, 117 at 5 and at 8).
+constexpr int kStart = 5;
 constexpr int kBlock = 64;                 // tokens that share a scale; the header's ATTN_CACHE_BLOCK
 
 struct Problem {
@@ -37,44 +41,38 @@ struct Problem {
     if (seen > all) seen = all;
     return seen > 0 ? (int)((seen + kBlock - 1) / kBlock) : 0;
   }
-  SHARES_FN int cost(int b, int t) const {
-    const int n = blocks(b, t);
-    return n > 0 ? n : 1;
-  }
+  SHARES_FN int cost(int b, int t) const { return kStart + blocks(b, t); }
 };
+
+// Units of a call, counted in int: below this (where the entry point refuses the call), so that sums of two stay in range.
+constexpr double kUnitLimit = 1073741824.0;
 
 struct Segment {
   int b, h, t;
-  long long begin;                         // of its blocks in the whole list
-  int blocks, cost;
+  int begin;                               // of its units in the whole list
+  int blocks;
+  SHARES_FN int end() const { return begin + kStart + blocks; }
+  SHARES_FN int block_at(int pos) const {  // the first block at or behind a unit of it
+    const int i = pos - begin - kStart;
+    return i > 0 ? i : 0;
+  }
 };
 
-// The segment that block `pos` of the list belongs to.  before(item): cost of the items (b, t), item = b * tiles + t, in front of
-// one, for one head; it is called with 0 .. B * tiles.
-template <class F> SHARES_FN Segment locate(const Problem& q, F&& before, int B, int H_kv, long long pos) {
-  Segment s;
-  s.b = 0;
-  for (int hi = B; hi - s.b > 1;) {        // the last sequence that begins at or before pos
-    const int mid = s.b + (hi - s.b) / 2;
-    if (H_kv * before(mid * q.tiles) <= pos) s.b = mid; else hi = mid;
-  }
-  const long long first = before(s.b * q.tiles), each = before((s.b + 1) * q.tiles) - first;
-  long long rest = pos - H_kv * first;
-  s.h = (int)(rest / each);
-  rest -= s.h * each;
-  s.t = 0;
-  for (int hi = q.tiles; hi - s.t > 1;) {
-    const int mid = s.t + (hi - s.t) / 2;
-    if (before(s.b * q.tiles + mid) - first <= rest) s.t = mid; else hi = mid;
-  }
-  s.begin = pos - (rest - (before(s.b * q.tiles + s.t) - first));
-  s.blocks = q.blocks(s.b, s.t);
-  s.cost = s.blocks > 0 ? s.blocks : 1;
-  return s;
+// Does unit `pos` of the list belong to item (b, t) of some head?  Of the units of one head, `first` stand in front of sequence b, `each` are b's,
+// and `at` of those stand in front of tile t.  If so, *s is the segment.  Exactly one item says yes: all are asked at once.
+SHARES_FN bool locate(const Problem& q, int b, int t, int first, int each, int at, int H_kv, int pos, Segment* s) {
+  int rest = pos - H_kv * first;
+  if (rest < at || rest - at >= H_kv * each) return false;          // (not in front of the item in the first head, nor behind b)
+  const int h = rest / each;
+  rest -= h * each;
+  const int blocks = q.blocks(b, t);
+  if (rest < at || rest >= at + kStart + blocks) return false;
+  *s = Segment{b, h, t, pos - (rest - at), blocks};
+  return true;
 }
 // The one behind it; there is one.
 SHARES_FN void next_segment(const Problem& q, int H_kv, Segment& s) {
-  s.begin += s.cost;
+  s.begin = s.end();
   if (++s.t == q.tiles) {
     s.t = 0;
     if (++s.h == H_kv) {
@@ -83,23 +81,33 @@ SHARES_FN void next_segment(const Problem& q, int H_kv, Segment& s) {
     }
   }
   s.blocks = q.blocks(s.b, s.t);
-  s.cost = s.blocks > 0 ? s.blocks : 1;
 }
 
-// Shares that `total` blocks are worth, and where share w begins.
-SHARES_FN int shares_of(long long total, int most, int least_blocks) {
-  const long long s = total / least_blocks;
-  return s < 1 ? 1 : s > most ? most : (int)s;
+// `total` units shared out: the first `longer` shares have one more than `each`.
+struct Shares {
+  int number, each, longer;
+  SHARES_FN int begin(int w) const { return w * each + (w < longer ? w : longer); }
+  // the first share that begins at or behind unit `pos`
+  SHARES_FN int at_or_behind(int pos) const {
+    const int edge = longer * (each + 1);
+    return pos <= edge ? (pos + each) / (each + 1) : longer + (pos - edge + each - 1) / each;
+  }
+};
+SHARES_FN Shares shares_of(int total, int most, int least) {
+  const int n = total / least;
+  Shares s;
+  s.number = n < 1 ? 1 : n > most ? most : n;
+  s.each = total / s.number;
+  s.longer = total - s.each * s.number;
+  return s;
 }
-SHARES_FN long long share_begin(long long total, int shares, int w) { return total * w / shares; }
 // What share w >= 1, which begins in s, notes for the joining kernel: parts of s, in shares w - 1 and the following; 0 where it is not the
 // first to begin inside s.  Note 0 holds the number of shares in `parts`.
 struct alignas(16) Join { int b, h, t, parts; };
-SHARES_FN Join join_of(long long total, int shares, int w, const Segment& s) {
+SHARES_FN Join join_of(const Shares& all, int w, const Segment& s) {
   Join j{s.b, s.h, s.t, 0};
-  if (w == 0) j.parts = shares;
-  else if (s.begin < share_begin(total, shares, w) && share_begin(total, shares, w - 1) <= s.begin)
-    j.parts = (int)(((s.begin + s.cost) * shares + total - 1) / total) - (w - 1);     // up to the first share that begins at its end or later
+  if (w == 0) j.parts = all.number;
+  else if (s.begin < all.begin(w) && all.begin(w - 1) <= s.begin) j.parts = all.at_or_behind(s.end()) - (w - 1);
   return j;
 }
 // Slot of part i of them.
@@ -121,18 +129,22 @@ struct CacheForm {
   // notes, then slots
   size_t workspace_bytes(int d) const { return split && shares > 1 ? shares * sizeof(Join) + 2 * (size_t)shares * slot_floats(d) * sizeof(float) : 0; }
 };
-template <int KW> constexpr int kLeastBlocks = KW == 4 ? 4 : 8;
+// No share is smaller: one block for each of the waves that share the blocks out; eight where they share them.
+template <int KW> constexpr int kLeastUnits = kStart + (KW == 4 ? 1 : 8);
+inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
+  return (double)B * H_kv * f.tiles * (kStart + capacity / kBlock);
+}
 inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
   const long long rows = (long long)N * (H / H_kv);
   CacheForm f;
-  f.RT = rows <= 16 ? 1 : 2;
-  f.KW = rows <= 32 ? 4 : 1;
+  f.RT = rows <= 64 ? 1 : 2;
+  f.KW = rows <= 16 ? 4 : 1;
   f.tiles = (int)((rows + f.rows() - 1) / f.rows());
   const int nb = capacity / kBlock;
   f.split = nb > 16 || f.tiles > 65535;    // (the grid's second dimension)
-  const double blocks = (double)B * H_kv * f.tiles * nb / (f.KW == 4 ? kLeastBlocks<4> : kLeastBlocks<1>);
+  const double most_shares = cache_units(B, H_kv, f, capacity) / (f.KW == 4 ? kLeastUnits<4> : kLeastUnits<1>);
   const int most = d == 256 ? 256 : 512;
-  f.shares = blocks >= most ? most : blocks < 1 ? 1 : (int)blocks;
+  f.shares = most_shares >= most ? most : most_shares < 1 ? 1 : (int)most_shares;
   f.many_parts = f.shares > 4.0 * B * H_kv * f.tiles;
   return f;
 }

@@ -47,7 +47,7 @@ def _values(c):
     k = c.K.double().cpu().numpy()
     v = c.V.double().cpu().transpose(3, 4).reshape(B, Hkv, cap, d).numpy()
     with np.errstate(divide="ignore", invalid="ignore"):
-        e = [np.round(np.log2(s.double().cpu().numpy())) for s in (c.K_scale, c.V_scale)]
+        e = [np.round(np.log2(np.abs(s.double().cpu().numpy()))) for s in (c.K_scale, c.V_scale)]
     return (k, v), e
 
 
@@ -76,6 +76,10 @@ class Pair:
                 for w in range(2):
                     assert np.array_equal(exponents[w][b, h, :blocks], ref.exponents[w][:blocks]), (b, h, w)
                     assert np.array_equal(values[w][b, h, :length], ref.values[w][:length], equal_nan=True), (b, h, w)
+                # the sign of V's scale: NaN in the block (or among tokens it held when they were appended)
+                marked = (self.dev.V_scale[b, h, :blocks] < 0).cpu().numpy()
+                nan = np.array([np.isnan(ref.values[1][64 * j:min(length, 64 * j + 64)]).any() for j in range(blocks)], dtype=bool)
+                assert np.array_equal(marked, nan) and (self.dev.K_scale[b, h, :blocks] > 0).all()
 
 
 # ---- append
@@ -300,7 +304,7 @@ def test_every_code_and_scale(lib):
         c.K.view(torch.uint8)[0, 0, 0] = codes.to(DEV)
         c.V.view(torch.uint8)[0, 0, 0, :, 0] = codes.to(DEV)
         c.K_scale.fill_(2.0 ** e)
-        c.V_scale.fill_(2.0 ** e)
+        c.V_scale.fill_(-(2.0 ** e))                       # there is NaN, among the codes and behind the token
         q = torch.zeros(1, 1, 1, 256, dtype=torch.bfloat16, device=DEV)
         c.K.view(torch.uint8)[0, 0, 0, 127] = c.K.view(torch.uint8)[0, 0, 0, 255] = 0
         O, lse = binding.attn_cache_fwd(q, c, _i32([1]), 1.0)
@@ -434,6 +438,9 @@ def _check_evict(c, weights, lengths, budget, recent, out=None):
                     continue
                 x, e = oracle.gathered(ref, which, want)
                 assert exps[b, h, :len(e)].tolist() == e
+                if which == 1:
+                    marked = [any(c.V_scale[b, h, t // 64] < 0 for t in want[lo:lo + 64]) for lo in range(0, n, 64)]
+                    assert (got.V_scale[b, h, :len(e)] < 0).tolist() == marked
                 assert np.array_equal(values[b, h, :n], x, equal_nan=True)
                 assert (values[b, h, n:-(-n // 64) * 64] == 0).all()
     return got, w, kept
@@ -445,6 +452,8 @@ def test_evict(lib, d):
     B, Hkv, cap = 4, 2, 448
     lengths = [448, 300, 100, 0]
     c = _filled(g, B, Hkv, cap, d, lengths)
+    c.V.view(torch.uint8)[0, 1, 2, 5, 7] = 0x7f            # a NaN in token 135
+    c.V_scale[0, 1, 2] *= -1
     for budget, recent in ((100, 20), (300, 300), (65, 0), (1, 1), (1, 0), (447, 63), (448, 5)):
         w = torch.exp(2 * torch.randn((B, Hkv, cap), generator=g)).to(DEV)
         out = None

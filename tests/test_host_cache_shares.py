@@ -12,6 +12,7 @@ HEADER_DIR = os.path.join(ROOT, "paper_2510_04212_amd", "csrc")
 MAIN = r"""
 #include "cache_shares.hpp"
 #include <cstdio>
+#include <cstdlib>
 #include <map>
 #include <tuple>
 #include <vector>
@@ -24,11 +25,27 @@ int main() {
     for (int& x : counts) scanf("%d", &x);
     const int tiles = (N * group + M - 1) / M;
     const Problem q{lengths.data(), counts[0] == -9 ? nullptr : counts.data(), capacity, N, group, causal, tiles, M};
-    std::vector<long long> sums{0};
+    std::vector<int> sums{0};
     for (int i = 0; i < B * tiles; ++i) sums.push_back(sums.back() + q.cost(i / tiles, i % tiles));
-    auto before = [&](int item) { return sums.at(item); };
-    const long long total = H * sums.back();
-    const int shares = shares_of(total, most, least);
+    auto locate_one = [&](int pos) {
+      Segment found{-1, 0, 0, 0, 0};
+      int times = 0;
+      for (int i = 0; i < B * tiles; ++i) {
+        const int b = i / tiles, first = sums.at(b * tiles);
+        Segment s;
+        if (locate(q, b, i % tiles, first, sums.at((b + 1) * tiles) - first, sums[i] - first, H, pos, &s)) { found = s; ++times; }
+      }
+      if (times != 1) { printf("found %d times\n", times); exit(1); }
+      return found;
+    };
+    const int total = H * sums.back();
+    const Shares all = shares_of(total, most, least);
+    const int shares = all.number;
+    if (shares < 1 || shares > most || all.begin(0) != 0 || all.begin(shares) != total) { printf("shares\n"); return 1; }
+    for (int pos = 0; pos <= total; pos += 1 + total / 1000) {
+      const int s = all.at_or_behind(pos);
+      if (s < 0 || s > shares || all.begin(s) < pos || (s > 0 && all.begin(s - 1) >= pos)) { printf("at or behind\n"); return 1; }
+    }
     std::vector<int> seen(shares, 0);
     for (int g = 0; g < (shares + 7) / 8 * 8; ++g)
       if (const int w = share_of(g, shares); w >= 0) ++seen.at(w);
@@ -37,17 +54,17 @@ int main() {
     std::map<std::tuple<int, int, int>, std::vector<int>> slots;
     std::vector<int> used(2 * shares, 0);
     for (int w = 0; w < shares; ++w) {
-      long long pos = share_begin(total, shares, w);
-      const long long end = share_begin(total, shares, w + 1);
+      int pos = all.begin(w);
+      const int end = all.begin(w + 1);
       if (end <= pos) { printf("empty share\n"); return 1; }
-      Segment s = locate(q, before, B, H, pos);
+      Segment s = locate_one(pos);
       while (true) {
-        if (s.b >= B || s.h >= H || s.t >= tiles || s.begin > pos || s.begin + s.cost <= pos) { printf("wrong segment\n"); return 1; }
+        if (s.b >= B || s.h >= H || s.t >= tiles || s.begin > pos || s.end() <= pos) { printf("wrong segment\n"); return 1; }
         if (s.blocks != q.blocks(s.b, s.t) || s.blocks > capacity / kBlock) { printf("wrong blocks\n"); return 1; }
-        const long long to = end < s.begin + s.cost ? end : s.begin + s.cost;
+        const int to = end < s.end() ? end : s.end();
         const auto key = std::make_tuple(s.b, s.h, s.t);
-        parts[key].push_back({(int)(pos - s.begin), (int)(to - s.begin)});
-        if (pos != s.begin || to != s.begin + s.cost) {
+        parts[key].push_back({s.block_at(pos), s.block_at(to)});
+        if (pos != s.begin || to != s.end()) {
           const int slot = 2 * w + (pos == s.begin ? 1 : 0);
           ++used.at(slot);
           slots[key].push_back(slot);
@@ -61,14 +78,14 @@ int main() {
     if ((long long)parts.size() != (long long)B * H * tiles) { printf("segments missing\n"); return 1; }
     for (auto& [key, list] : parts) {
       int at = 0;
-      for (auto [from, to] : list) { if (from != at || to <= from) { printf("hole\n"); return 1; } at = to; }
-      if (at != q.cost(std::get<0>(key), std::get<2>(key))) { printf("end missing\n"); return 1; }
+      for (auto [from, to] : list) { if (from != at || to < from) { printf("hole\n"); return 1; } at = to; }
+      if (at != q.blocks(std::get<0>(key), std::get<2>(key))) { printf("end missing\n"); return 1; }
     }
     // the joining kernel's view: the notes of shares 1 ..
     std::map<std::tuple<int, int, int>, int> joined;
     for (int w = 0; w < shares; ++w) {
-      const Segment s = locate(q, before, B, H, share_begin(total, shares, w));
-      const Join j = join_of(total, shares, w, s);
+      const Segment s = locate_one(all.begin(w));
+      const Join j = join_of(all, w, s);
       if (w == 0 && j.parts != shares) { printf("first note\n"); return 1; }
       if (w == 0 || j.parts == 0) continue;
       const auto key = std::make_tuple(j.b, j.h, j.t);
@@ -117,7 +134,7 @@ def test_every_block_is_taken_once_and_every_part_joined(tmp_path_factory):
         # lengths and counts as a caller may hold them, valid or not
         lengths = [rng.choice((0, 1, 63, 64, 65, capacity - 1, capacity, capacity + 1, rng.randint(0, capacity), -5, 2**31 - 1)) for _ in range(B)]
         counts = [-9] * B if rng.random() < 0.5 else [rng.choice((0, 1, N, rng.randint(0, N), -3, 2**31 - 1)) for _ in range(B)]
-        cases.append([B, H, N, group, rng.randint(0, 1), capacity, M, rng.choice((1, 3, 8, 100, 512)), rng.choice((1, 4, 8))] + lengths + counts)
+        cases.append([B, H, N, group, rng.randint(0, 1), capacity, M, rng.choice((1, 3, 8, 100, 512, 768)), rng.choice((1, 4, 6, 13))] + lengths + counts)
     r = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True)
     assert r.returncode == 0, r.stdout[-200:] + r.stderr[-500:]
     assert r.stdout.count("ok") == len(cases)
@@ -134,8 +151,8 @@ def test_the_form_covers_the_rows_and_the_workspace_is_what_the_library_says(tmp
     for c, line in zip(cases, out.splitlines()):
         RT, KW, tiles, shares, split, slot, many = map(int, line.split())
         rows, M = c[3] * c[1] // c[2], 64 * RT // KW
-        assert tiles * M >= rows > (tiles - 1) * M and 1 <= shares <= 512
+        assert tiles * M >= rows > (tiles - 1) * M and 1 <= shares <= 768
         assert binding.cache_fwd_workspace_bytes(*c) == (16 * shares + 2 * shares * slot * 4 if split and shares > 1 else 0)
         kinds.add((RT, KW, bool(split)))
         many_parts.add((RT, KW, bool(many)))
-    assert kinds == many_parts == {(RT, KW, s) for RT, KW in ((1, 4), (2, 4), (2, 1)) for s in (False, True)}
+    assert kinds == many_parts == {(RT, KW, s) for RT, KW in ((1, 4), (1, 1), (2, 1)) for s in (False, True)}
