@@ -481,6 +481,13 @@ def attn_bwd_rect(Q, K, V, O, dO, LSE, causal, softmax_scale, variant=STANDARD, 
 
 # ---- rotary positions and the 8-bit cache
 
+try:
+    from . import _operators            # plain calls, marshalled in C++; None (False) from it: not a plain call, handled here
+except ImportError as e:
+    raise ImportError("the plain calls' marshalling is missing or does not fit this torch: build it with "
+                      "`python -m paper_2510_04212_amd.build`") from e
+
+_PLAIN = (torch.Tensor, torch.nn.Parameter)
 CACHE_BLOCK = 64
 _ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
@@ -549,6 +556,10 @@ def attn_rope(Q, K=None, frequencies=None, positions=None, interleaved=False, ma
     Q [B,H,N,d], K [B,H_kv,N,d] with any strides; frequencies: rope_frequencies(...)[0]; positions: int32 [N] or [B,N], the default 0 .. N-1.
     Outputs are new tensors laid out like the inputs, or Q_out, K_out, which may be Q and K themselves.  inverse: rotates back, which is the
     backward pass (autograd.rope has both)."""
+    if Q_out is None and K_out is None and stream is None and type(Q) in _PLAIN and frequencies is not None:
+        out = _operators.rope(Q, K, frequencies, positions, interleaved, magnitude, inverse)
+        if out is not None:
+            return out
     B, H, N, d = _rows(Q, "Q")
     device = Q.device
     H_kv = 0
@@ -622,6 +633,8 @@ def attn_cache_append(cache, K, V, lengths, counts=None, stream=None):
 
     lengths: int32 [B], the tokens of each sequence in its cache, the new ones among them; counts: int32 [B], how many of the N tokens (the
     first ones) a sequence really has; all where absent."""
+    if stream is None and _operators.cache_append(*cache, K, V, lengths, counts):
+        return
     B, H_kv, capacity, d, device = _cache_shape(cache)
     if _rows(K, "K") != _rows(V, "V") or (K.shape[0], K.shape[1], K.shape[3]) != (B, H_kv, d):
         raise ValueError("K and V must be [B,H_kv,N,d] with the sequences, heads and head size of the cache")
@@ -650,6 +663,10 @@ def attn_cache_fwd(Q, cache, lengths, softmax_scale, causal=True, counts=None, O
 
     workspace: a CUDA tensor of at least cache_fwd_workspace_bytes(...) bytes; allocated when absent.  Calls that may overlap in time (two
     streams, two graphs) need one each."""
+    if O is None and LSE is None and workspace is None and stream is None:
+        out = _operators.cache_fwd(*cache, Q, lengths, softmax_scale, causal, counts)
+        if out is not None:
+            return out
     B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
     _sequence_lengths(lengths, counts, B, device)
     if O is None:
@@ -679,6 +696,10 @@ def attn_cache_weights(Q, cache, LSE, lengths, softmax_scale, causal=True, count
 
     weights: what tokens got before (the call's own tokens had none: not read for them); None: nothing.  out: where the result goes, `weights`
     itself for instance; a new tensor when absent.  Positions past a sequence's end become 0."""
+    if stream is None:
+        result = _operators.cache_weights(*cache, Q, LSE, lengths, softmax_scale, causal, counts, weights, out)
+        if result is not None:
+            return result if out is None else out
     B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
     _sequence_lengths(lengths, counts, B, device)
     _dense(LSE, "LSE", (B, H, N), torch.float32, device)
@@ -700,6 +721,10 @@ def attn_cache_evict(cache, weights, lengths, budget, recent, out=None, stream=N
     weights: float32 [B,H_kv,capacity] of attn_cache_weights.  out: another Cache with room for `budget` tokens; a new one of the least
     capacity when absent.  weights_out: float32 [B,H_kv,capacity of out], the kept tokens' weights, then 0.  kept: int32
     [B,H_kv,budget], their old positions, then -1.  The caller's lengths are then lengths.clamp(max=budget)."""
+    if stream is None and out is not None:
+        result = _operators.cache_evict(*cache, weights, lengths, *out, budget, recent)
+        if result is not None:
+            return (out, *result)
     B, H_kv, capacity, d, device = _cache_shape(cache)
     _dense(weights, "weights", (B, H_kv, capacity), torch.float32, device)
     _sequence_lengths(lengths, None, B, device)

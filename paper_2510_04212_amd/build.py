@@ -1,9 +1,10 @@
 """Builds the HIP library in-tree:  python -m paper_2510_04212_amd.build
 
-One hipcc invocation per source (gfx950 only).  Three libraries come out:
+One hipcc invocation per source (gfx950 only).  Four libraries come out:
   libattn_gfx950.so         the attention library (the C ABI of include/attn.h);
   libattn_probe_gfx950.so   measurement aids that only the benchmark loads (csrc/probe.h);
-  _autograd.so              the autograd node of attention() (host code, linked against the first).
+  _autograd.so              the autograd node of attention() (host code, linked against the first);
+  _operators.so             plain calls of the rotary positions and the 8-bit cache (the same).
 Packed-fp32 code generation is switched off for all device code.
 """
 import os
@@ -15,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libattn_gfx950.so")
 PROBE_LIB = os.path.join(HERE, "libattn_probe_gfx950.so")
-NODE_LIB = os.path.join(HERE, "_autograd.so")
+NODES = ["autograd", "operators"]              # csrc/NAME.cpp -> _NAME.so
 SOURCES = ["api.hip", "fwd.hip", "delta.hip", "bwd.hip", "api_cache.hip", "rope.hip", "cache.hip", "cache_attn.hip"]
 PROBE_SOURCES = ["probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -38,15 +39,15 @@ EXTRA_FLAGS = {"bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"], "fwd.hip
                "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
-def _node_command():
-    """One g++ call: csrc/autograd.cpp against torch's C++ interface."""
+def _node_command(name):
+    """One g++ call: csrc/NAME.cpp against torch's C++ interface."""
     import torch
     root = os.path.dirname(torch.__file__)
     return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
             + [a for p in (os.path.join(root, "include"), os.path.join(root, "include/torch/csrc/api/include"),
                            sysconfig.get_paths()["include"], "/opt/rocm/include") for a in ("-isystem", p)]
-            + [os.path.join(CSRC, "autograd.cpp"), "-o", NODE_LIB, "-L" + HERE, "-l:" + os.path.basename(LIB),
+            + [os.path.join(CSRC, name + ".cpp"), "-o", os.path.join(HERE, f"_{name}.so"), "-L" + HERE, "-l:" + os.path.basename(LIB),
                "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(root, "lib"),
                "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10"])
 
@@ -76,10 +77,15 @@ def build(verbose=True):
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
-    cmd = _node_command()
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    procs = []
+    for name in NODES:
+        cmd = _node_command(name)
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        procs.append((cmd, subprocess.Popen(cmd)))
+    for cmd, p in procs:
+        if p.wait() != 0:
+            raise subprocess.CalledProcessError(p.returncode, cmd)
     return LIB
 
 
