@@ -6,12 +6,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-DEVI unsigned max_over_wave(unsigned x) {
-#pragma unroll
-  for (int i = 32; i; i >>= 1) x = max(x, (unsigned)__shfl_xor((int)x, i));
-  return x;
-}
-
 // ---- append.  One work-group per (sequence, head, block of the cache that gets tokens): it alone reads and writes that
 // block and its scales.  With amax the largest finite magnitude of the block's new tokens, the block's exponent is
 //   e = max(exponent_for(amax), e of the tokens that are already in it),
@@ -148,10 +142,14 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_append_k
 // ---- evict, first kernel: which tokens stay.  One work-group per (sequence, head).  The need-th largest of the weights in front of
 // the recent tokens is found digit by digit (11, 11 and 10 bits of an order-preserving integer form) with a histogram in LDS, then the
 // tokens above it and the first of those equal to it are written in ascending order: positions are prefix counts.
+//
+// Bound by latency (a work-group has a head's weights for itself): keys stay in LDS, loaded once, where ROOM holds them, and loops are not
+// unrolled, as the first pass over an instruction costs more than the jump.  us of 8 heads of 32768 and 128 of 4400 weights: 43 and
+// 12.2 with the weights read again in every pass, 30 and 20 with the keys in registers and all loops unrolled, SELECT_US so.
 constexpr int kSelectThreads = 1024;
 constexpr int kBins = 2048;
 
-// larger weight <=> larger key; -0 = +0, NaN above everything
+// larger weight <=> larger key; -0 = +0, NaN above everything.  No weight's key is below that of -infinity, 0x7fffff.
 DEVI unsigned sort_key(float w) {
   const unsigned u = __float_as_uint(w);
   if (w != w) return 0xffffffffu;
@@ -159,32 +157,12 @@ DEVI unsigned sort_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// inclusive sum over the work-group in thread order; every thread gets the total as well
-DEVI unsigned scan_sum(unsigned x, unsigned* waves, unsigned& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
-    const unsigned y = (unsigned)__shfl_up((int)x, i);
-    if (lane >= i) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) waves[wave] = x;
-  __syncthreads();
-  unsigned before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kSelectThreads / 64; ++w) {
-    if (w < wave) before += waves[w];
-    total += waves[w];
-  }
-  return x + before;
-}
-
-__global__ __launch_bounds__(kSelectThreads) void attn_cache_select_kernel(EvictArgs p) {
+template <int ROOM> __global__ __launch_bounds__(kSelectThreads) void attn_cache_select_kernel(EvictArgs p) {
+  __shared__ u32x4 keys[ROOM / 4];
   __shared__ unsigned bins[kBins];
-  __shared__ unsigned waves[kSelectThreads / 64];
+  __shared__ unsigned waves[2][kSelectThreads / 64];
   __shared__ unsigned found[2];
-  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
+  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const size_t bh = (size_t)b * p.H_kv + h;
   int* kept = p.kept + bh * p.budget;
   const int length = min(max(p.lengths[b], 0), p.from.capacity);
@@ -197,7 +175,30 @@ __global__ __launch_bounds__(kSelectThreads) void attn_cache_select_kernel(Evict
   const int old = length - p.recent, need = p.budget - p.recent;      // need < old
   for (int i = tid; i < p.recent; i += kSelectThreads) kept[need + i] = old + i;
   if (need == 0) return;
-  const float* weights = p.weights + bh * p.from.capacity;
+  const f32x4* weights = reinterpret_cast<const f32x4*>(p.weights + bh * p.from.capacity);       // (rows of a multiple of 64)
+  // Four keys to a thread at a time, whole work-groups of them: behind the last, keys are 0, which is no weight's, falls into the lowest bin, and is
+  // neither above nor equal to one that is looked for.
+  const int quads = (old + 4 * kSelectThreads - 1) / (4 * kSelectThreads) * kSelectThreads;
+  auto from_memory = [&](int quad) {
+    u32x4 k{0, 0, 0, 0};
+    if (4 * quad < old) {
+      const f32x4 w = weights[quad];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[i] = 4 * quad + i < old ? sort_key(w[i]) : 0u;
+    }
+    return k;
+  };
+  static_assert(ROOM % (4 * kSelectThreads) == 0, "whole work-groups of keys");
+  const bool stays = old <= ROOM;          // the keys do
+  auto key = [&](int quad) { return stays ? keys[quad] : from_memory(quad); };
+  if (stays) {
+#pragma unroll 4
+    for (int i = tid; i < quads; i += kSelectThreads) keys[i] = from_memory(i);
+  }
+  auto sum_before = [&](const unsigned* of_waves) {        // of the waves in front of this one
+    const unsigned x = sum_to_lane(lane < wave ? of_waves[lane & (kSelectThreads / 64 - 1)] : 0u);
+    return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+  };
 
   unsigned prefix = 0, known = 0;                          // the digits found so far, and the bits they cover
   unsigned left = (unsigned)need;                          // wanted among the keys that have these digits
@@ -207,16 +208,31 @@ __global__ __launch_bounds__(kSelectThreads) void attn_cache_select_kernel(Evict
     const unsigned digits = pass == 2 ? 1023u : 2047u;
     for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
     __syncthreads();
-    for (int i = tid; i < old; i += kSelectThreads) {
-      const unsigned key = sort_key(weights[i]);
-      if ((key & known) == prefix) atomicAdd(&bins[(key >> shift) & digits], 1u);
+#pragma unroll 1
+    for (int quad = tid; quad < quads; quad += kSelectThreads) {
+      const u32x4 k = key(quad);
+      // keys that differ in a digit before: nothing to count, as for nearly all of them in the later passes
+      if (__all(((k[0] ^ prefix) & known) != 0 && ((k[1] ^ prefix) & known) != 0 && ((k[2] ^ prefix) & known) != 0 && ((k[3] ^ prefix) & known) != 0))
+        continue;
+      // a wave of equal keys adds to one bin at once
+      const unsigned leader = (unsigned)__builtin_amdgcn_readfirstlane((int)k[0]);
+      if (__all(((k[0] ^ leader) | (k[1] ^ leader) | (k[2] ^ leader) | (k[3] ^ leader)) == 0)) {
+        if (lane == 0) atomicAdd(&bins[(leader >> shift) & digits], 256u);
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (((k[i] ^ prefix) & known) == 0) atomicAdd(&bins[(k[i] >> shift) & digits], 1u);
     }
     __syncthreads();
     // from the top: thread t holds bins (2047 - 2t) and the one below
     const int top = kBins - 1 - 2 * tid;
     const unsigned upper = bins[top], lower = bins[top - 1];
-    unsigned total;
-    const unsigned to = scan_sum(upper + lower, waves, total), from = to - upper - lower;
+    unsigned to = sum_to_lane(upper + lower);
+    if (lane == 63) waves[0][wave] = to;
+    __syncthreads();
+    to += sum_before(waves[0]);
+    const unsigned from = to - upper - lower;
     if (from < left && left <= to) {
       const bool in_upper = left <= from + upper;
       found[0] = (unsigned)(in_upper ? top : top - 1);
@@ -226,97 +242,135 @@ __global__ __launch_bounds__(kSelectThreads) void attn_cache_select_kernel(Evict
     prefix |= found[0] << shift;
     known |= digits << shift;
     left = found[1];
-    __syncthreads();
   }
-  // key == prefix: of these the first `left` stay
-  unsigned above = 0, equal = 0;                           // before the present stretch
-  for (int i0 = 0; i0 < old; i0 += 4 * kSelectThreads) {
-    const int i = i0 + 4 * tid;
-    unsigned more[4], same[4], count = 0;                  // (above, equal) as 16 + 16 bits: 4096 at most each
+  // key == prefix: of these the first `left` stay.  kSelectThreads quads at a time; the counts' exchange alternates between two places.
+  unsigned above = 0, equal = 0;                           // in front of them
+#pragma unroll 1
+  for (int first = 0, odd = 0; first < quads; first += kSelectThreads, odd ^= 1) {
+    const int quad = first + tid;
+    unsigned count = 0;                                    // (above, equal) as 16 + 16 bits: 4096 at most each
+    const u32x4 k = key(quad);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned key = i + j < old ? sort_key(weights[i + j]) : 0u;
-      more[j] = i + j < old && key > prefix;
-      same[j] = i + j < old && key == prefix;
-      count += more[j] | same[j] << 16;
-    }
-    unsigned total;
-    const unsigned before = scan_sum(count, waves, total) - count;
-    unsigned a = above + (before & 0xffffu), e = equal + (before >> 16);
+    for (int i = 0; i < 4; ++i) count += (k[i] > prefix ? 1u : 0u) + (k[i] == prefix ? 0x10000u : 0u);
+    const unsigned to = sum_to_lane(count);
+    if (lane == 63) waves[odd][wave] = to;
+    __syncthreads();
+    const unsigned x = to - count + sum_before(waves[odd]);
+    unsigned a = above + (x & 0xffffu), e = equal + (x >> 16);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (more[j] || (same[j] && e < left)) kept[a + min(e, left)] = i + j;
-      a += more[j];
-      e += same[j];
+    for (int i = 0; i < 4; ++i) {
+      const bool bigger = k[i] > prefix, tie = k[i] == prefix;
+      if (bigger || (tie && e < left)) kept[a + min(e, left)] = 4 * quad + i;
+      a += bigger;
+      e += tie;
     }
-    above += total & 0xffffu;
-    equal += total >> 16;
+    if (tid == kSelectThreads - 1) {
+      bins[2 * odd] = a;
+      bins[2 * odd + 1] = e;
+    }
+    __syncthreads();
+    above = bins[2 * odd];
+    equal = bins[2 * odd + 1];
   }
 }
 
 // ---- evict, second kernel: one work-group per block of the new cache.  Its scales are the largest of its tokens' old ones, so that
-// codes are only ever multiplied by powers of two <= 1.  V's codes are gathered one by one (its blocks hold columns).
+// codes are only ever multiplied by powers of two <= 1.  V's blocks hold columns: of each, four tokens' codes are picked from 8 bytes where the four
+// lie so near each other (nearly all do while most tokens stay), and one by one elsewhere.  Bound by bytes.
+//
+// Two loads one after the other, the kept positions and what they lead to: all of a thread's codes are on their way before anything waits.
 template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_gather_kernel(EvictArgs p) {
   const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x, tid = threadIdx.x;
   const size_t bh = (size_t)b * p.H_kv + h;
-  const int stay = min(min(max(p.lengths[b], 0), p.from.capacity), p.budget);
-  const int here = min(stay - j * kBlock, kBlock);         // tokens of this block
-  __shared__ int source[kBlock];
+  const int* kept = p.kept + bh * p.budget + j * kBlock;
+  const int room = min(p.budget - j * kBlock, kBlock);     // of the list: -1 behind the last kept token
+  auto source = [&](int t) { return t < room ? kept[t] : -1; };
+  constexpr int CH = D / 16, NK = (kBlock * CH + kThreads - 1) / kThreads, NV = D / 16;
+  const int u = tid & 15;
+  int from_k[NK], from_v[4];
+#pragma unroll
+  for (int k = 0; k < NK; ++k) from_k[k] = source((tid + k * kThreads) / CH);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) from_v[i] = source(4 * u + i);
+  const int one = tid < kBlock ? source(tid) : -1;
+
+  const unsigned char* K = p.from.K + bh * p.from.capacity * D;
+  const unsigned char* V = p.from.V + bh * p.from.capacity * D;
+  u32x4 xk[NK];
+#pragma unroll
+  for (int k = 0; k < NK; ++k) {
+    xk[k] = u32x4{0, 0, 0, 0};
+    if (from_k[k] >= 0) xk[k] = *reinterpret_cast<const u32x4*>(K + (size_t)from_k[k] * D + (tid + k * kThreads) % CH * 16);
+  }
+  const int first = max(from_v[0], 0), window = min(first % kBlock & ~3, kBlock - 8);       // of the source block's tokens: 8 from here
+  unsigned pick = 0;                       // of those, v_perm's selector: 12 is a zero
+  bool near = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool real = from_v[i] >= 0;
+    const int at = from_v[i] % kBlock - window;
+    near &= !real || (from_v[i] / kBlock == first / kBlock && at < 8);
+    pick |= (real ? (unsigned)(at & 7) : 12u) << (8 * i);
+  }
+  unsigned lo[NV], hi[NV];
+  if (near) {
+    const unsigned char* eight = V + (size_t)(first / kBlock) * (D * kBlock) + (tid >> 4) * kBlock + window;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const unsigned* at = reinterpret_cast<const unsigned*>(eight + k * (kThreads / 16) * kBlock);
+      lo[k] = at[0];
+      hi[k] = at[1];
+    }
+  }
+  // scales: the largest of the block's tokens', and what each token's codes are multiplied by
   __shared__ float times[2][kBlock];
-  __shared__ int moved[2];                                 // does any code change?
+  __shared__ int moved[2];                 // does any code change?
   if (tid < kBlock) {
-    const bool real = tid < here;
-    const int t = real ? p.kept[bh * p.budget + j * kBlock + tid] : 0;
-    if (p.weights_out)
-      p.weights_out[bh * p.to.capacity + j * kBlock + tid] = real ? p.weights[bh * p.from.capacity + t] : 0.f;
-    const size_t at = bh * (p.from.capacity / kBlock) + t / kBlock;
+    const bool real = one >= 0;
+    const size_t at = bh * (p.from.capacity / kBlock) + max(one, 0) / kBlock;
     const float vs = real ? p.from.V_scale[at] : 0.f;      // (its sign: NaN among the block's codes)
     const int ek = real ? exponent(p.from.K_scale[at]) : -127, ev = real ? exponent(vs) : -127;
+    if (p.weights_out) p.weights_out[bh * p.to.capacity + j * kBlock + tid] = real ? p.weights[bh * p.from.capacity + one] : 0.f;
     const bool nan = __any(vs < 0.f);
     const int mk = (int)max_over_wave((unsigned)(ek + 127)) - 127, mv = (int)max_over_wave((unsigned)(ev + 127)) - 127;
-    source[tid] = t;
     times[0][tid] = power(max(ek - mk, -126));
     times[1][tid] = power(max(ev - mv, -126));
-    const bool any_k = __any(real && ek != mk), any_v = __any(real && ev != mv);
-    if (tid == 0 && here > 0) {
+    const bool any_k = __any(real && ek != mk), any_v = __any(real && ev != mv), any = __any(real);
+    if (tid == 0) {
       moved[0] = any_k;
       moved[1] = any_v;
-      const size_t to = bh * (p.to.capacity / kBlock) + j;
-      p.to.K_scale[to] = power(mk);
-      p.to.V_scale[to] = nan ? -power(mv) : power(mv);
-    }
-  }
-  if (here <= 0) return;
-  __syncthreads();
-  const unsigned char* K = p.from.K + bh * p.from.capacity * D;
-  unsigned char* K_to = p.to.K + (bh * p.to.capacity + j * kBlock) * D;
-  constexpr int CH = D / 16;
-#pragma unroll
-  for (int k = 0; k < (kBlock * CH + kThreads - 1) / kThreads; ++k) {
-    const int v = tid + k * kThreads, t = v / CH, c = v % CH;
-    if (v >= kBlock * CH) break;
-    u32x4 w{0, 0, 0, 0};
-    if (t < here) {
-      w = *reinterpret_cast<const u32x4*>(K + (size_t)source[t] * D + c * 16);
-      if (moved[0]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = rescale4_e4m3(w[i], times[0][t]);
+      if (any) {
+        const size_t to = bh * (p.to.capacity / kBlock) + j;
+        p.to.K_scale[to] = power(mk);
+        p.to.V_scale[to] = nan ? -power(mv) : power(mv);
       }
     }
-    *reinterpret_cast<u32x4*>(K_to + t * D + c * 16) = w;
   }
-  const unsigned char* V = p.from.V + bh * p.from.capacity * D;
+  __syncthreads();
+  if (room <= 0 || kept[0] < 0) return;    // a block behind the last kept token stays as it is
+  unsigned char* K_to = p.to.K + (bh * p.to.capacity + j * kBlock) * D;
   unsigned char* V_to = p.to.V + (bh * p.to.capacity + j * kBlock) * D;
-  const int u = tid & 15;
-  size_t from[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) from[i] = (size_t)(source[4 * u + i] / kBlock) * (D * kBlock) + source[4 * u + i] % kBlock;
-#pragma unroll 4
-  for (int c = tid >> 4; c < D; c += kThreads / 16) {
+  for (int k = 0; k < NK; ++k) {
+    const int v = tid + k * kThreads, t = v / CH;
+    if (v >= kBlock * CH) break;
+    if (moved[0]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xk[k][i] = rescale4_e4m3(xk[k][i], times[0][t]);
+    }
+    *reinterpret_cast<u32x4*>(K_to + t * D + v % CH * 16) = xk[k];
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (tid >> 4) + k * (kThreads / 16);
     unsigned w = 0;
+    if (near) {
+      w = __builtin_amdgcn_perm(hi[k], lo[k], pick);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * u + i < here) w |= (unsigned)V[from[i] + c * kBlock] << (8 * i);
+      for (int i = 0; i < 4; ++i)
+        if (from_v[i] >= 0) w |= (unsigned)V[(size_t)(from_v[i] / kBlock) * (D * kBlock) + c * kBlock + from_v[i] % kBlock] << (8 * i);
+    }
     if (moved[1])
       w = pack4_e4m3(__builtin_amdgcn_cvt_f32_fp8((int)w, 0) * times[1][4 * u], __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * times[1][4 * u + 1],
                      __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * times[1][4 * u + 2], __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * times[1][4 * u + 3]);
@@ -346,7 +400,10 @@ hipError_t attn_cache_append_dispatch(const AppendArgs& p, int d, hipStream_t st
 }
 
 hipError_t attn_cache_evict_dispatch(const EvictArgs& p, int d, hipStream_t stream) {
-  attn_cache_select_kernel<<<dim3((unsigned)p.H_kv, (unsigned)p.B), kSelectThreads, 0, stream>>>(p);
+  // room for the longest sequence's keys if there is any, so that as many work-groups as possible share a compute unit
+  const dim3 heads((unsigned)p.H_kv, (unsigned)p.B);
+  if (p.from.capacity <= 8192) attn_cache_select_kernel<8192><<<heads, kSelectThreads, 0, stream>>>(p);
+  else attn_cache_select_kernel<32768><<<heads, kSelectThreads, 0, stream>>>(p);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const dim3 grid((unsigned)(p.to.capacity / kBlock), (unsigned)p.H_kv, (unsigned)p.B);
   return by_head_size(d, [&](auto D) {

@@ -74,6 +74,21 @@ hipError_t attn_cache_evict_dispatch(const EvictArgs&, int d, hipStream_t);
 // they bound a read.
 DEVI int real_count(const int* counts, int b, int N) { return counts ? min(max(counts[b], 0), N) : N; }
 
+// Scans over a wave in lane order by row shifts (1, 2, 4, 8 lanes within 16) and row broadcasts: vector instructions, no LDS exchange.  join(0, x) = x.
+template <class F> DEVI unsigned scan_wave(unsigned x, F&& join) {
+  x = join(__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false), x);
+  x = join(__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false), x);
+  x = join(__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false), x);
+  x = join(__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false), x);
+  x = join(__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false), x);      // the last lane of row 0 to row 1, of 2 to 3
+  x = join(__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false), x);      // lane 31 to rows 2 and 3
+  return x;
+}
+DEVI unsigned sum_to_lane(unsigned x) { return scan_wave(x, [](unsigned a, unsigned b) { return a + b; }); }
+DEVI unsigned max_over_wave(unsigned x) {       // the same in all lanes
+  return (unsigned)__builtin_amdgcn_readlane((int)scan_wave(x, [](unsigned a, unsigned b) { return max(a, b); }), 63);
+}
+
 // 2^e as float32, e >= -126, and the exponent of a scale
 DEVI float power(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 DEVI int exponent(float scale) { return (int)((__float_as_uint(scale) >> 23) & 255) - 127; }

@@ -126,11 +126,7 @@ DEVI int scan_units(const Problem& q, int items, int run, Runs& runs) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int x = 0;
   for (int i = tid * run; i < min(items, (tid + 1) * run); ++i) x += q.cost(i / q.tiles, i % q.tiles);
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
-    const int y = __shfl_up(x, i);
-    if (lane >= i) x += y;
-  }
+  x = (int)sum_to_lane((unsigned)x);
   if (lane == 63) runs.waves[wave] = x;
   __syncthreads();
 #pragma unroll
