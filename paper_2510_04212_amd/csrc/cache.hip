@@ -127,14 +127,17 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_append_k
     if (!fills && !whole_v) continue;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      unsigned* to = reinterpret_cast<unsigned*>(V + (c * 8 + i) * kBlock + 4 * u);
+      unsigned char* to = V + (c * 8 + i) * kBlock + 4 * u;
       unsigned w = pack4_e4m3(bf16_at(xv[k][0], i) * to_v, bf16_at(xv[k][1], i) * to_v, bf16_at(xv[k][2], i) * to_v,
                               bf16_at(xv[k][3], i) * to_v) & fills;
-      if (fills != 0xffffffffu) {
-        if (!whole_v) w |= *to & ~fills;
-        else if (keeps) w |= rescale4_e4m3(*to, times_v) & keeps;
+      if (whole_v || fills == 0xffffffffu) {
+        if (keeps) w |= rescale4_e4m3(*reinterpret_cast<unsigned*>(to), times_v) & keeps;
+        *reinterpret_cast<unsigned*>(to) = w;
+      } else {                             // single bytes: nothing has to be read first
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (fills >> (8 * j) & 0xffu) to[j] = (unsigned char)(w >> (8 * j));
       }
-      *to = w;
     }
   }
 }
@@ -145,7 +148,7 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_append_k
 //
 // Bound by latency (a work-group has a head's weights for itself): keys stay in LDS, loaded once, where ROOM holds them, and loops are not
 // unrolled, as the first pass over an instruction costs more than the jump.  us of 8 heads of 32768 and 128 of 4400 weights: 43 and
-// 12.2 with the weights read again in every pass, 30 and 20 with the keys in registers and all loops unrolled, SELECT_US so.
+// 12.2 with the weights read again in every pass, 30 and 20 with the keys in registers and all loops unrolled, 22.8 and 8.8 so.
 constexpr int kSelectThreads = 1024;
 constexpr int kBins = 2048;
 

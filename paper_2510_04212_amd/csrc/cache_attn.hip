@@ -659,88 +659,202 @@ template <int D> hipError_t launch_fwd(const AttendArgs& p, hipStream_t stream) 
 }
 
 // ---- weights.  The wave's tile is S^T again: lane (r, g) adds up exp(S - LSE) of row r of every row tile for the 16 tokens of its
-// group, and the 16 lanes of a group are added at the end.  A block's tokens belong to one wave (WG = false: few row tiles) or to
-// one work-group whose four waves take the row tiles in turn: no atomics.
-template <int D, bool WG> __global__ __launch_bounds__(kThreads, 2) void attn_cache_weights_kernel(WeighArgs p) {
-  __shared__ float joined[WG ? 4 : 1][kBlock];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int r = lane & 15, g = lane >> 4;
-  const int nb = p.cache.capacity / kBlock;
-  const int blk = WG ? blockIdx.x : blockIdx.x * 4 + wave, h = blockIdx.y, b = blockIdx.z;
-  if (blk >= nb) return;
-  const size_t bh = (size_t)b * p.H_kv + h;
-  const int n = real_count(p.counts, b, p.N), rows = n * p.group;
-  const long long length = p.lengths[b];
-  const int all = (int)max(0ll, min(length, (long long)p.cache.capacity));
-  const int t0 = blk * kBlock;
-  float sum[16];
+// group, and the 16 lanes of a group are added at the end: a block's tokens belong to one wave or one work-group, no atomics.
+//
+// Few row tiles: bound by K's bytes; a wave takes up to 8 blocks one after the other, the next one's codes on their way (one token of 32
+// sequences of 2000 to 4160 tokens, H 32/8, d 128: 25 us with a block per wave, 22.6 with 2, 21.4 with 8).  Many: by the exponentials and the products, and by what a row
+// tile costs besides (addresses, loads), which two blocks share (500 queries, H 32/8, over 16384 tokens: 157 us with one block, 102 with two);
+// the four waves of a work-group take the row tiles in turn.
+DEVI float sum_over_16_lanes(float x) {        // the same in all 16: four rotations of the row
+  x += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, false));
+  x += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x124, 0xf, 0xf, false));
+  x += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x122, 0xf, 0xf, false));
+  x += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x121, 0xf, 0xf, false));
+  return x;
+}
+// What a (sequence, head) is to a wave.
+struct Weighed {
+  int b, h, n, rows, all;                  // queries, rows of the list; tokens in the cache
+  long long length;
+  size_t first;                            // element of weights of the head's first token
+  DEVI Weighed(const WeighArgs& p, int b_, int h_) : b(b_), h(h_) {
+    n = uniform(real_count(p.counts, b, p.N));
+    rows = n * p.group;
+    length = uniform(p.lengths[b]);
+    all = (int)max(0ll, min(length, (long long)p.cache.capacity));
+    first = ((size_t)b * p.H_kv + h) * p.cache.capacity;
+  }
+  // what token t had: one of this call's has no weight yet
+  DEVI float had(const WeighArgs& p, int t) const { return p.in && t < all && t < length - n ? p.in[first + t] : 0.f; }
+};
+// one row tile's queries: fragments, LSE in units of log 2, tokens that the lane's row sees (none where it is not there or sees nothing)
+template <int D> struct QueryTile {
+  bf16x8 q[D / 32];
+  float less;
+  int limit;
+  DEVI void load(const WeighArgs& p, const Weighed& x, bool there, int query, int member, int g) {
+    const int head = x.h * p.group + (there ? member : 0), i = there ? query : 0;
+    const unsigned short* at = p.Q.at + x.b * p.Q.sb + head * p.Q.sh + i * p.Q.sn;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  if (t0 < all && rows > 0) {
-    KCodes<D> k;
-    const unsigned token = (r >> 2) * 16 + (r & 3);
-    k.load(p.cache.K + (bh * p.cache.capacity + t0) * D, token * D + g * 16, token * D + g * 8);
-    const float k_scale = p.cache.K_scale[bh * nb + blk], scale_log2 = p.scale * kLog2e;
-    bf16x8 kf[4][D / 32];
+    for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const bf16x8*>(at + query_column<D>(c, g));
+    const float lse = p.LSE[((size_t)x.b * p.H + head) * p.N + i];
+    limit = there && lse != -INFINITY ? (p.causal ? (int)max(0ll, min((long long)x.all, x.length - x.n + i + 1)) : x.all) : 0;
+    less = limit > 0 ? lse * kLog2e : 0.f;
+  }
+};
+template <int D> DEVI void widen_keys(bf16x8 (&kf)[4][D / 32], const KCodes<D>& k, float scale) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c)
-        kf[i][c] = c < 2 * Cols<D>::C64 ? key_frag(k.c[i][c / 2], c & 1, k_scale) : widen8(k.odd[i].x, k.odd[i].y, k_scale);
-    // the first row that sees the block's first token
-    const long long from = p.causal ? max(0ll, t0 - (length - n)) * p.group : 0;
-    for (long long tile = from / 16 + (WG ? wave : 0); tile * 16 < rows; tile += WG ? 4 : 1) {
-      const int row = (int)(tile * 16) + r;
-      const bool there = row < rows;
-      const int query = there ? row / p.group : 0, head = h * p.group + (there ? row - query * p.group : 0);
-      const unsigned short* at = p.Q.at + b * p.Q.sb + head * p.Q.sh + query * p.Q.sn;
-      bf16x8 qf[D / 32];
+    for (int c = 0; c < D / 32; ++c)
+      kf[j][c] = c < 2 * Cols<D>::C64 ? key_frag(k.c[j][c / 2], c & 1, scale) : widen8(k.odd[j].x, k.odd[j].y, scale);
+}
+// a row tile's probabilities for the 16 tokens from `seen_from` on
+template <int D> DEVI void add_weights(float (&sum)[16], const bf16x8 (&kf)[4][D / 32], const QueryTile<D>& tile, float scale_log2, int seen_from) {
+  const int seen = tile.limit - seen_from;
+  const bool whole = __all(seen >= 16);
+  f32x4 s[4];
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(at + query_column<D>(c, g));
-      const float lse = p.LSE[((size_t)b * p.H + head) * p.N + query];
-      const long long seen = p.causal ? min((long long)all, length - n + query + 1) : all;
-      // a row that is not there, or sees nothing, adds nothing
-      const int limit = there && lse != -INFINITY ? (int)max(0ll, seen) : 0;
-      const float less = limit > 0 ? lse * kLog2e : 0.f;
+  for (int j = 0; j < 4; ++j) s[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f32x4 s{0, 0, 0, 0};
+  for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) s = mfma16(kf[i][c], qf[c], s);
+    for (int j = 0; j < 4; ++j) s[j] = mfma16(kf[j][c], tile.q[c], s[j]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c], scale_log2, -less));
-          sum[4 * i + c] += t0 + 16 * g + 4 * i + c < limit ? x : 0.f;
+  for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], scale_log2, -tile.less));
+  if (!whole) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i >= seen) s[i / 4][i % 4] = 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum[i] += s[i / 4][i % 4];
+}
+// of token 16 g + r: the sum over the 16 lanes that have some of it
+DEVI float own_sum(const float (&sum)[16], int r) {
+  float mine = 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float x = sum_over_16_lanes(sum[j]);
+    mine = r == j ? x : mine;
+  }
+  return mine;
+}
+
+template <int D> __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_weights_few_kernel(WeighArgs p, int per_wave) {
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+  const int nb = p.cache.capacity / kBlock, first = uniform((int)(blockIdx.x * 4 + wave) * per_wave);
+  if (first >= nb) return;
+  const Weighed x(p, blockIdx.z, blockIdx.y);
+  const int end = min(nb, first + per_wave);
+  const int keys_end = x.rows > 0 ? min(end, (x.all + kBlock - 1) / kBlock) : first;       // blocks with something to add
+  const unsigned token = (r >> 2) * 16 + (r & 3);
+  const unsigned char* K = p.cache.K + x.first * D;
+  const float* Ks = p.cache.K_scale + x.first / kBlock;
+  KCodes<D> k;
+  float k_scale = 0.f, had = x.had(p, first * kBlock + lane);
+  QueryTile<D> tile;
+  auto load_key = [&](int blk) {
+    if (blk >= keys_end) return;
+    k_scale = Ks[blk];
+    k.load(K + (size_t)blk * (kBlock * D), token * D + g * 16, token * D + g * 8);
+  };
+  auto load_tile = [&](int row) { tile.load(p, x, row < x.rows, row / p.group, row % p.group, g); };
+  load_key(first);
+  if (first < keys_end) load_tile(r);
+  const float scale_log2 = p.scale * kLog2e;
+#pragma unroll 1
+  for (int blk = first; blk < end; ++blk) {
+    const int t = blk * kBlock + lane;
+    float sum[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+    const float was = had;
+    if (blk + 1 < end) had = x.had(p, t + kBlock);
+    if (blk < keys_end) {
+      bf16x8 kf[4][D / 32];
+      widen_keys<D>(kf, k, k_scale);
+      load_key(blk + 1);
+      add_weights<D>(sum, kf, tile, scale_log2, blk * kBlock + 16 * g);
+      if (x.rows > 16) {
+        for (int row = 16; row < x.rows; row += 16) {
+          load_tile(row + r);
+          add_weights<D>(sum, kf, tile, scale_log2, blk * kBlock + 16 * g);
         }
+        load_tile(r);
       }
     }
+    const float mine = own_sum(sum, r);
+    p.out[x.first + t] = t >= x.all ? 0.f : was + mine;
   }
-  float mine = 0.f;                                        // of token 16 g + r
+}
+
+template <int D, int NB> __global__ __launch_bounds__(kThreads, 2) void attn_cache_weights_many_kernel(WeighArgs p) {
+  __shared__ float joined[4][NB * kBlock];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
+  const int nb = p.cache.capacity / kBlock, blk = blockIdx.x * NB, t0 = blk * kBlock;
+  const Weighed x(p, blockIdx.z, blockIdx.y);
+  float sum[NB][16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float x = sum[i];
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d);
-    mine = r == i ? x : mine;
+    for (int j = 0; j < 16; ++j) sum[i][j] = 0.f;
+  if (t0 < x.all && x.rows > 0) {
+    const unsigned token = (r >> 2) * 16 + (r & 3);
+    // rows from the tile of the first that sees the first of these tokens on
+    const long long hidden = p.causal ? max(0ll, t0 - (x.length - x.n)) * p.group : 0;
+    constexpr int kStep = 64;
+    int row = (int)min(hidden / 16 * 16, (long long)x.rows) + wave * 16 + r;
+    int query = row / p.group, member = row - query * p.group;
+    const int step_query = kStep / p.group, step_member = kStep - step_query * p.group;
+    QueryTile<D> next;
+    auto load_tile = [&]() {                               // and on to the one after it
+      next.load(p, x, row < x.rows, query, member, g);
+      row += kStep;
+      query += step_query;
+      member += step_member;
+      if (member >= p.group) {
+        member -= p.group;
+        ++query;
+      }
+    };
+    int tile = uniform(row - r);
+    bf16x8 kf[NB][4][D / 32];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int from = min(blk + i, nb - 1);               // a block past the end: the last one again, for nothing
+      KCodes<D> k;
+      k.load(p.cache.K + (x.first + (size_t)from * kBlock) * D, token * D + g * 16, token * D + g * 8);
+      widen_keys<D>(kf[i], k, p.cache.K_scale[x.first / kBlock + from]);
+    }
+    const float scale_log2 = p.scale * kLog2e;
+    if (tile < x.rows) load_tile();
+    for (; tile < x.rows; tile += kStep) {
+      const QueryTile<D> now = next;
+      if (tile + kStep < x.rows) load_tile();
+#pragma unroll
+      for (int i = 0; i < NB; ++i) add_weights<D>(sum[i], kf[i], now, scale_log2, t0 + i * kBlock + 16 * g);
+    }
   }
-  if constexpr (WG) {
-    joined[wave][lane] = mine;
-    __syncthreads();
-    if (wave != 0) return;
-    mine = joined[0][lane] + joined[1][lane] + joined[2][lane] + joined[3][lane];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) joined[wave][i * kBlock + lane] = own_sum(sum[i], r);
+  __syncthreads();
+  for (int i = wave; i < NB && blk + i < nb; i += 4) {
+    const int at = i * kBlock + lane, t = t0 + at;
+    p.out[x.first + t] = t >= x.all ? 0.f : x.had(p, t) + joined[0][at] + joined[1][at] + joined[2][at] + joined[3][at];
   }
-  const int t = t0 + lane;
-  const size_t at = bh * p.cache.capacity + t;
-  // a token of this call's has no weight yet
-  p.out[at] = t >= all ? 0.f : (p.in && t < length - n ? p.in[at] : 0.f) + mine;
 }
 
 template <int D> hipError_t launch_weights(const WeighArgs& p, hipStream_t stream) {
   const unsigned nb = (unsigned)(p.cache.capacity / kBlock);
-  if ((long long)p.N * p.group <= 64)
-    attn_cache_weights_kernel<D, false><<<dim3((nb + 3) / 4, (unsigned)p.H_kv, (unsigned)p.B), kThreads, 0, stream>>>(p);
-  else
-    attn_cache_weights_kernel<D, true><<<dim3(nb, (unsigned)p.H_kv, (unsigned)p.B), kThreads, 0, stream>>>(p);
+  constexpr int NB = D <= 128 ? 2 : 1;       // (a lane's registers hold one block's keys of d = 256)
+  if ((long long)p.N * p.group <= 64) {
+    // a block per wave until the waves are two to a SIMD, then more, up to 8
+    const long long blocks = (long long)p.B * p.H_kv * nb;
+    const unsigned per_wave = (unsigned)std::min(8ll, std::max(1ll, blocks / 2048)), per_group = 4 * per_wave;
+    attn_cache_weights_few_kernel<D><<<dim3((nb + per_group - 1) / per_group, (unsigned)p.H_kv, (unsigned)p.B), kThreads, 0, stream>>>(p, (int)per_wave);
+  } else
+    attn_cache_weights_many_kernel<D, NB><<<dim3((nb + NB - 1) / NB, (unsigned)p.H_kv, (unsigned)p.B), kThreads, 0, stream>>>(p);
   return hipGetLastError();
 }
 
