@@ -350,7 +350,7 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
 constexpr int kBuffers = 4;
 template <int D, int RT, int KW> constexpr int kWavesPerSimd = D == 256 ? 1 : 2;
 template <int D, int RT, int KW, bool SPLIT>
-__global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares) {
+__global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
   constexpr int RG = 4 / KW, M = 16 * RT * RG;
   static_assert(KW == 1 || KW == 4, "the four waves have rows of their own, or blocks");
   __shared__ Runs runs;
@@ -366,15 +366,17 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
 
   Segment seg;
   int pos, end, w = 0;
+  Shares all{1, 0, 0};
+  Join* notes = reinterpret_cast<Join*>(p.partials);
   if constexpr (SPLIT) {
     const int items = p.B * tiles, run = (items + kThreads - 1) / kThreads;
-    const Shares all = shares_of(p.H_kv * scan_units(q, items, run, runs), most_shares, kLeastUnits<KW>);
+    all = shares_of(p.H_kv * scan_units(q, items, run, runs), most_shares, kLeastUnits<KW>);
     w = share_of(blockIdx.x, all.number);
     if (w < 0) return;
     pos = uniform(all.begin(w));
     end = uniform(all.begin(w + 1));
     seg = find_segment(q, p.B, p.H_kv, run, pos, runs);
-    if (tid == 0) reinterpret_cast<Join*>(p.partials)[w] = join_of(all, w, seg);
+    if (tid == 0 && !notes_by_segment) notes[w] = note_of_share(all, w, seg, p.H_kv, tiles);
   } else {
     seg.b = blockIdx.z;
     seg.h = blockIdx.x;
@@ -388,6 +390,8 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
 
   while (true) {
     const int to = min(end, seg.end());
+    if (SPLIT && notes_by_segment && tid == 0 && pos == seg.begin)
+      notes[segment_number(seg, p.H_kv, tiles)] = note_of_segment(all, w, seg, p.H_kv, tiles);
     const int b = seg.b, h = seg.h, first_row = seg.t * M + rg * RT * 16;
     const int blk0 = seg.block_at(pos), blk_end = seg.block_at(to);
     const size_t bh = (size_t)b * p.H_kv + h;
@@ -559,20 +563,21 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
   }
 }
 
-// Joins the parts of a segment that was split between shares: the work-group of the first share that begins inside it.  blockIdx.y is one row tile
-// of 16 and DT of the D / 16 column tiles; the NW waves take every NW-th part, kAhead of them in flight, and join theirs in LDS.
+// Joins the parts of the segments that were split between shares.  blockIdx.x is a note; blockIdx.y one row tile of 16 and DT of the D / 16 column
+// tiles; the NW waves take every NW-th part, kAhead of them in flight, and join theirs in LDS.
 template <int D, int RT, int KW, int NW, int DT>
-__global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p, int shares_room) {
-  constexpr int RG = 4 / KW, M = 16 * RT * RG, PARTS = D / 16 / DT, kAhead = DT <= 2 ? 4 : 1;
+__global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p, int tiles, int shares_room, bool notes_by_segment) {
+  constexpr int RG = 4 / KW, M = 16 * RT * RG, PARTS = D / 16 / DT, kAhead = NW == 16 ? 8 : DT <= 8 ? 2 : 1;
   __shared__ f32x4 joined[NW][DT][64];
   __shared__ float joined_ml[2][NW][16];
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
   const int r = lane & 15, g = lane >> 4;
-  const int w = blockIdx.x + 1;
+  const int note = blockIdx.x + (notes_by_segment ? 0 : 1);
   const Join* notes = reinterpret_cast<const Join*>(p.partials);
   const int shares = notes[0].parts;
-  const Join j = notes[w];                 // there is room for it, whether there is such a share or not
-  if (w >= shares || j.parts == 0) return;
+  const Join j = notes[note];              // there is room for it, whether there is such a share or not
+  if ((!notes_by_segment && note >= shares) || j.parts == 0) return;
+  const int b = j.segment / tiles / p.H_kv, h = j.segment / tiles % p.H_kv, t = j.segment % tiles;
   const float* slots = p.partials + shares_room * (sizeof(Join) / sizeof(float));
   const int tile = blockIdx.y / PARTS, dt0 = (blockIdx.y % PARTS) * DT;
 
@@ -585,19 +590,17 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p,
     float mp[kAhead], lp[kAhead];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
-      const bool there = part + a * NW < j.parts;
-      const float* slot = slots + (size_t)joined_slot(w, there ? part + a * NW : part) * kSlotFloats<D, RT, KW>;
+      mp[a] = -INFINITY;
+      lp[a] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) x[a][i] = f32x4{0, 0, 0, 0};
+      if (part + a * NW >= j.parts) continue;
+      const float* slot = slots + (size_t)joined_slot(j.first, part + a * NW) * kSlotFloats<D, RT, KW>;
       const float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;
 #pragma unroll
       for (int i = 0; i < DT; ++i) x[a][i] = reinterpret_cast<const f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + lane];
       mp[a] = ml[r];
       lp[a] = ml[16 + r];
-      if (!there) {                        // the same part again: it counts for nothing
-        mp[a] = -INFINITY;
-        lp[a] = 0.f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) x[a][i] = f32x4{0, 0, 0, 0};
-      }
     }
     float most = m;
 #pragma unroll
@@ -634,21 +637,21 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p,
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] += joined[k][i][lane] * by;
   }
-  store_row<DT>(p, find_row(p, j.b, j.t * M + tile * 16 + r), j.b, j.h, o, most, l, dt0, g);
+  store_row<DT>(p, find_row(p, b, t * M + tile * 16 + r), b, h, o, most, l, dt0, g);
 }
 
 template <int D, int RT, int KW> hipError_t launch_fwd(const AttendArgs& p, const CacheForm& f, hipStream_t stream) {
   if (!f.split) {
-    attn_cache_fwd_kernel<D, RT, KW, false><<<dim3((unsigned)p.H_kv, (unsigned)f.tiles, (unsigned)p.B), kThreads, 0, stream>>>(p, f.tiles, 0);
+    attn_cache_fwd_kernel<D, RT, KW, false><<<dim3((unsigned)p.H_kv, (unsigned)f.tiles, (unsigned)p.B), kThreads, 0, stream>>>(p, f.tiles, 0, false);
     return hipGetLastError();
   }
-  attn_cache_fwd_kernel<D, RT, KW, true><<<(unsigned)((f.shares + 7) / 8 * 8), kThreads, 0, stream>>>(p, f.tiles, f.shares);
+  attn_cache_fwd_kernel<D, RT, KW, true><<<(unsigned)((f.shares + 7) / 8 * 8), kThreads, 0, stream>>>(p, f.tiles, f.shares, f.many_parts);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || f.shares == 1) return e;
   const unsigned joins = (unsigned)(f.shares - 1), row_tiles = (4 / KW) * RT;
   if (f.many_parts)
-    attn_cache_merge_kernel<D, RT, KW, 16, 2><<<dim3(joins, row_tiles * (D / 32)), 1024, 0, stream>>>(p, f.shares);
+    attn_cache_merge_kernel<D, RT, KW, 16, 2><<<dim3((unsigned)(p.B * p.H_kv * f.tiles), row_tiles * (D / 32)), 1024, 0, stream>>>(p, f.tiles, f.shares, true);
   else
-    attn_cache_merge_kernel<D, RT, KW, 2, D / 16><<<dim3(joins, row_tiles), 128, 0, stream>>>(p, f.shares);
+    attn_cache_merge_kernel<D, RT, KW, 2, D / 16><<<dim3(joins, row_tiles), 128, 0, stream>>>(p, f.tiles, f.shares, false);
   return hipGetLastError();
 }
 template <int D> hipError_t launch_fwd(const AttendArgs& p, hipStream_t stream) {

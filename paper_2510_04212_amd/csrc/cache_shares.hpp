@@ -4,7 +4,7 @@
 // begin and end one, then one for each of its key blocks.  `shares` work-groups take equal parts of all units, wherever segments begin and
 // end: sequences may differ in length by any factor, and lengths are known on the device only.  A part of a segment is left in the
 // workspace, in slot 2w + 1 of share w where it begins the segment, 2w otherwise (a share ends inside one segment and begins inside one at
-// most), and a second kernel joins the parts: the first share that begins inside a segment leaves a note for it (Join).
+// most), and a second kernel joins the parts, as the notes say that the shares leave for it (Join).
 //
 // Plain C++ (host and device).
 #pragma once
@@ -101,17 +101,24 @@ SHARES_FN Shares shares_of(int total, int most, int least) {
   s.longer = total - s.each * s.number;
   return s;
 }
-// What share w >= 1, which begins in s, notes for the joining kernel: parts of s, in shares w - 1 and the following; 0 where it is not the
-// first to begin inside s.  Note 0 holds the number of shares in `parts`.
-struct alignas(16) Join { int b, h, t, parts; };
-SHARES_FN Join join_of(const Shares& all, int w, const Segment& s) {
-  Join j{s.b, s.h, s.t, 0};
+// A note for the joining kernel: the segment's number in the list and its parts, in shares `first` and the following (none: it is whole).  Where segments
+// are more than a quarter of the shares, there is one note for each share, of the segment that it begins inside if it is the first to do so, and
+// note 0 holds the number of shares in `parts`; otherwise one for each segment, by the share that begins it.
+struct alignas(16) Join { int segment, first, parts, unused; };
+SHARES_FN int segment_number(const Segment& s, int H_kv, int tiles) { return (s.b * H_kv + s.h) * tiles + s.t; }
+SHARES_FN Join note_of_share(const Shares& all, int w, const Segment& s, int H_kv, int tiles) {
+  Join j{segment_number(s, H_kv, tiles), w - 1, 0, 0};
   if (w == 0) j.parts = all.number;
   else if (s.begin < all.begin(w) && all.begin(w - 1) <= s.begin) j.parts = all.at_or_behind(s.end()) - (w - 1);
   return j;
 }
-// Slot of part i of them.
-SHARES_FN int joined_slot(int w, int i) { return 2 * (w - 1 + i) + (i == 0 ? 1 : 0); }
+// share w begins s
+SHARES_FN Join note_of_segment(const Shares& all, int w, const Segment& s, int H_kv, int tiles) {
+  const int parts = all.at_or_behind(s.end()) - w;
+  return Join{segment_number(s, H_kv, tiles), w, parts > 1 ? parts : 0, 0};
+}
+// Slot of part i.
+SHARES_FN int joined_slot(int first, int i) { return 2 * (first + i) + (i == 0 ? 1 : 0); }
 // Share of a work-group, or -1: neighbours in the list go to one XCD (work-groups are dealt to the eight in turn), as they read the
 // same head's cache.  The grid has a multiple of 8 work-groups, at least `shares`.
 SHARES_FN int share_of(int group, int shares) {

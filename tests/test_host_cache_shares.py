@@ -81,19 +81,38 @@ int main() {
       for (auto [from, to] : list) { if (from != at || to < from) { printf("hole\n"); return 1; } at = to; }
       if (at != q.blocks(std::get<0>(key), std::get<2>(key))) { printf("end missing\n"); return 1; }
     }
-    // the joining kernel's view: the notes of shares 1 ..
+    // the joining kernel's view: the notes of shares 1 .., and those of all segments
+    auto key_of = [&](int number) { return std::make_tuple(number / tiles / H, number / tiles % H, number % tiles); };
     std::map<std::tuple<int, int, int>, int> joined;
-    for (int w = 0; w < shares; ++w) {
-      const Segment s = locate_one(all.begin(w));
-      const Join j = join_of(all, w, s);
-      if (w == 0 && j.parts != shares) { printf("first note\n"); return 1; }
-      if (w == 0 || j.parts == 0) continue;
-      const auto key = std::make_tuple(j.b, j.h, j.t);
-      ++joined[key];
+    auto check = [&](const Join& j) {
+      ++joined[key_of(j.segment)];
       std::vector<int> mine;
-      for (int i = 0; i < j.parts; ++i) mine.push_back(joined_slot(w, i));
-      if (mine != slots[key]) { printf("other parts joined\n"); return 1; }
+      for (int i = 0; i < j.parts; ++i) mine.push_back(joined_slot(j.first, i));
+      if (mine != slots[key_of(j.segment)]) { printf("other parts joined\n"); exit(1); }
+    };
+    std::map<std::tuple<int, int, int>, Join> of_segment;
+    for (int w = 0; w < shares; ++w) {
+      int pos = all.begin(w);
+      const int end = all.begin(w + 1);
+      Segment s = locate_one(pos);
+      const Join j = note_of_share(all, w, s, H, tiles);
+      if (w == 0 && j.parts != shares) { printf("first note\n"); return 1; }
+      if (w > 0 && j.parts > 0) check(j);
+      while (true) {
+        if (pos == s.begin) of_segment[std::make_tuple(s.b, s.h, s.t)] = note_of_segment(all, w, s, H, tiles);
+        pos = end < s.end() ? end : s.end();
+        if (pos >= end) break;
+        next_segment(q, H, s);
+      }
     }
+    if ((long long)of_segment.size() != (long long)B * H * tiles) { printf("notes missing\n"); return 1; }
+    auto once = joined;
+    joined.clear();
+    for (auto& [key, j] : of_segment) {
+      if (key_of(j.segment) != key || (j.parts == 0) != (slots.count(key) == 0)) { printf("wrong note\n"); return 1; }
+      if (j.parts > 0) check(j);
+    }
+    if (joined != once) { printf("notes differ\n"); return 1; }
     for (auto& [key, list] : slots) if (joined[key] != 1) { printf("not joined once\n"); return 1; }
     if (joined.size() != slots.size()) { printf("joined for nothing\n"); return 1; }
     printf("ok %d\n", shares);
