@@ -225,9 +225,6 @@ DEVI void store_row(const AttendArgs& p, const Row& x, int b, int h, const f32x4
   if (dt0 == 0 && g == 0) p.LSE[((size_t)b * p.H + head) * p.N + x.query] = x.empty ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// every load but the n youngest has landed (s_waitcnt vmcnt(n))
-template <int n> DEVI void wait_vmem_but() { __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14); }
-
 // bytes of w that are 0x7f or 0xff, E4M3's NaN: 0x80 in each of them
 DEVI unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
@@ -270,9 +267,13 @@ DEVI void take_out_nan(Acc<D, RT>& a, VCodes<D>& v, const int (&limit)[RT], int 
 // The maximum that probabilities are taken relative to is let fall behind the true one by up to kSlack (a factor of 2^kSlack, harmless in float32 and
 // bf16 alike), so that the accumulators are hardly ever rescaled.
 constexpr float kSlack = 8.f;
+//
+// Two tiles of rows: of the two waves that share a SIMD, the one that multiplies goes first, so that the other's softmax fills in (2048 queries over
+// 16384 tokens 632 -> 600 us; d = 64, 4096 queries of 4 sequences 463 -> 422; with one wave a SIMD, d = 256, 243 -> 248, not there).
 template <int D, int RT, class F>
 DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, float scale_log2,
                      const int (&limit)[RT], bool masked, int t0, int g, F&& after_scores) {
+  constexpr bool kMultipliesFirst = RT == 2 && D < 256;
   f32x4 s[RT][4];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
@@ -297,6 +298,7 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
       for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][D / 32 - 1], s[rt][i]);
     }
   }
+  if (kMultipliesFirst) __builtin_amdgcn_s_setprio(0);
   after_scores();
   if (masked) {
 #pragma unroll
@@ -331,6 +333,7 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
         pr[rt][j][e] = (bf16_t)x;
       }
   }
+  if (kMultipliesFirst) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
     const u32x4 w = v.c[dt];
@@ -346,8 +349,8 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
 //
 // KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead.  KW = 1, many rows: bound by
-// the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers kBuffers - 1 blocks ahead.
-constexpr int kBuffers = 4;
+// the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers a block ahead (three blocks ahead, in four
+// buffers: 16 queries of 64 sequences of 4300 tokens, H 32/8, d 128, 139 us; one ahead, in two: 125.  2048 queries over 16384: 636 and 620).
 template <int D, int RT, int KW> constexpr int kWavesPerSimd = D == 256 ? 1 : 2;
 template <int D, int RT, int KW, bool SPLIT>
 __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
   __shared__ Runs runs;
   __shared__ f32x4 joined[KW == 4 ? 4 * RT * (D / 16) * 64 : 1];         // [wave][RT][D / 16][lane]
   __shared__ float joined_m[KW == 4 ? 4 * RT * 16 : 1], joined_l[KW == 4 ? 4 * RT * 16 : 1];
-  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? kBuffers * Staged<D>::kBytes : 16];
+  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? 2 * Staged<D>::kBytes : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int kw = wave % KW, rg = wave / KW;
@@ -462,18 +465,11 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) settle(qf[rt][c]);
-#pragma unroll
-      for (int i = 1; i < kBuffers - 1; ++i)
-        if (blk0 + i < blk_end) fetch(blk0 + i, i);
       int buffer = 0;
       for (int blk = blk0; blk < blk_end; ++blk) {
-        static_assert(kBuffers == 4, "transfers behind this block's: two blocks' at most");
-        const int behind = blk_end - 1 - blk;
-        if (behind >= 2) wait_vmem_but<2 * MINE>();
-        else if (behind == 1) wait_vmem_but<MINE>();
-        else wait_vmem();
+        wait_vmem();
         __syncthreads();                                   // this block has landed for all waves, and all have read the one before
-        if (behind >= kBuffers - 1) fetch(blk + kBuffers - 1, (buffer + kBuffers - 1) % kBuffers);
+        if (blk + 1 < blk_end) fetch(blk + 1, buffer ^ 1);
         if (rows_here) {
           if (blk > blk0 && ((blk - blk0) & 63) == 0) load_scales(blk);
           const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), (blk - blk0) & 63));
@@ -484,7 +480,7 @@ __global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cac
           block_step<D, RT>(a, qf, k, v, ks, vs, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g,
                             [&] { read_staged<D>(v, base + in_piece); });
         }
-        buffer = (buffer + 1) % kBuffers;
+        buffer ^= 1;
       }
     } else {
       for (int blk = blk0 + kw; blk < blk_end; blk += KW) {

@@ -136,22 +136,35 @@ struct CacheForm {
   // notes, then slots
   size_t workspace_bytes(int d) const { return split && shares > 1 ? shares * sizeof(Join) + 2 * (size_t)shares * slot_floats(d) * sizeof(float) : 0; }
 };
-// No share is smaller: one block for each of the waves that share the blocks out; eight where they share them.
-template <int KW> constexpr int kLeastUnits = kStart + (KW == 4 ? 1 : 8);
+// No share is smaller.  Four waves that share the blocks out: one block; sharing them: two (20 rows of 4 sequences of 1000 tokens, H 32/8, d 128: 24.7 us
+// at eight blocks, 21.5 at four, 19.7 at two; 64 rows of 32768: 33.3, 28.7, 29.6; 8400 rows of 2100: 70.8, 73.6, 73.9).
+template <int KW> constexpr int kLeastUnits = kStart + (KW == 4 ? 1 : 2);
 inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
   return (double)B * H_kv * f.tiles * (kStart + capacity / kBlock);
 }
+// Rows.  Up to 16: each wave takes blocks of its own (one token of 64 sequences of 4300, H 32/8, d 128: 102 us, and 116 with the blocks
+// shared through LDS; of 4 sequences of 1000: 13 and 24).  From 17 on the blocks would be read and widened once for each row tile: the waves share
+// them (32 rows of 64 x 4300: 132 us with blocks of a wave's own, 118 shared; 64 rows: 164 and 123).  From 65 on two row tiles a wave (68 rows:
+// 284 us with one, 169 with two; 128 rows: 274 and 184).
+//
+// Split.  Sharing out costs 5 to 8 us (finding the segment, the second kernel) and pays where a segment is long for the work-groups that there are: beyond
+// 16 blocks, 32 where there is a segment for every work-group that runs at once, as they then fill the chip by themselves; for up to 16 rows, whose
+// blocks four waves share out, 32 from a sixteenth of that on, and 64.  Whole / split, us, full caches, H 32/8, d 128: one token, capacity 1024:
+// 1 sequence 8.8 / 14.8, 64 25.7 / 30.3; 2048: 1 15.6 / 14.5, 16 15.3 / 22.7; 4096: 1 25.0 / 13.3, 4 23 / 17, 64 91 / 98, and 60 / 66 at lengths of
+// 256 to 4096.  64 rows: 1024: 1 19 / 23; 2048: 4 33 / 24, 64 59 / 63; 4096: 4 61 / 28.  2048 queries of 2048 tokens 65 / 71, 4096 of 4096 197 / 175.
 inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
   const long long rows = (long long)N * (H / H_kv);
   CacheForm f;
   f.RT = rows <= 64 ? 1 : 2;
   f.KW = rows <= 16 ? 4 : 1;
   f.tiles = (int)((rows + f.rows() - 1) / f.rows());
-  const int nb = capacity / kBlock;
-  f.split = nb > 16 || f.tiles > 65535;    // (the grid's second dimension)
   const double most_shares = cache_units(B, H_kv, f, capacity) / (f.KW == 4 ? kLeastUnits<4> : kLeastUnits<1>);
-  const int most = d == 256 ? 256 : 512;
+  const int most = d == 256 ? 256 : 512;   // as many as run at once
+  const double segments = (double)B * H_kv * f.tiles;
+  int whole = segments >= most ? 32 : 16;
+  if (f.KW == 4 && segments >= most / 16) whole = segments >= most ? 64 : 32;
+  f.split = capacity / kBlock > whole || f.tiles > 65535;       // (the grid's second dimension)
   f.shares = most_shares >= most ? most : most_shares < 1 ? 1 : (int)most_shares;
-  f.many_parts = f.shares > 4.0 * B * H_kv * f.tiles;
+  f.many_parts = f.shares > 4 * segments;
   return f;
 }
