@@ -266,10 +266,10 @@ DEVI void take_out_nan(Acc<D, RT>& a, VCodes<D>& v, const int (&limit)[RT], int 
 //
 // The maximum that probabilities are taken relative to is let fall behind the true one by up to kSlack (a factor of 2^kSlack, harmless in float32 and
 // bf16 alike), so that the accumulators are hardly ever rescaled.
-constexpr float kSlack = 8.f;
 //
 // Two tiles of rows: of the two waves that share a SIMD, the one that multiplies goes first, so that the other's softmax fills in (2048 queries over
 // 16384 tokens 632 -> 600 us; d = 64, 4096 queries of 4 sequences 463 -> 422; with one wave a SIMD, d = 256, 243 -> 248, not there).
+constexpr float kSlack = 8.f;
 template <int D, int RT, class F>
 DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, float scale_log2,
                      const int (&limit)[RT], bool masked, int t0, int g, F&& after_scores) {
@@ -351,9 +351,8 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
 // KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead.  KW = 1, many rows: bound by
 // the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers a block ahead (three blocks ahead, in four
 // buffers: 16 queries of 64 sequences of 4300 tokens, H 32/8, d 128, 139 us; one ahead, in two: 125.  2048 queries over 16384: 636 and 620).
-template <int D, int RT, int KW> constexpr int kWavesPerSimd = D == 256 ? 1 : 2;
 template <int D, int RT, int KW, bool SPLIT>
-__global__ __launch_bounds__(kThreads, (kWavesPerSimd<D, RT, KW>)) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
   constexpr int RG = 4 / KW, M = 16 * RT * RG;
   static_assert(KW == 1 || KW == 4, "the four waves have rows of their own, or blocks");
   __shared__ Runs runs;
@@ -642,7 +641,7 @@ template <int D, int RT, int KW> hipError_t launch_fwd(const AttendArgs& p, cons
     return hipGetLastError();
   }
   attn_cache_fwd_kernel<D, RT, KW, true><<<(unsigned)((f.shares + 7) / 8 * 8), kThreads, 0, stream>>>(p, f.tiles, f.shares, f.many_parts);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess || f.shares == 1) return e;
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const unsigned joins = (unsigned)(f.shares - 1), row_tiles = (4 / KW) * RT;
   if (f.many_parts)
     attn_cache_merge_kernel<D, RT, KW, 16, 2><<<dim3((unsigned)(p.B * p.H_kv * f.tiles), row_tiles * (D / 32)), 1024, 0, stream>>>(p, f.tiles, f.shares, true);
@@ -847,7 +846,10 @@ template <int D, int NB> __global__ __launch_bounds__(kThreads, 2) void attn_cac
 template <int D> hipError_t launch_weights(const WeighArgs& p, hipStream_t stream) {
   const unsigned nb = (unsigned)(p.cache.capacity / kBlock);
   constexpr int NB = D <= 128 ? 2 : 1;       // (a lane's registers hold one block's keys of d = 256)
-  if ((long long)p.N * p.group <= 64) {
+  // The crossing point is where the second block's widened keys are paid for, later the more there are of them.  us, few / many, 32 sequences of 4096
+  // (d = 128; 16 of d = 32, 64; 8 of d = 256): 96 rows 75 / 119, 256 148 / 164, 384 204 / 211, 512 264 / 255, 1024 513 / 387; d = 32: 96 rows 19.2 / 19.7, 128
+  // 23.4 / 21.7; d = 64: 128 27 / 30, 192 37.4 / 37.7, 256 47 / 44; d = 256: 64 32 / 54, 512 132 / 152.
+  if ((long long)p.N * p.group <= 3 * D) {
     // a block per wave until the waves are two to a SIMD, then more, up to 8
     const long long blocks = (long long)p.B * p.H_kv * nb;
     const unsigned per_wave = (unsigned)std::min(8ll, std::max(1ll, blocks / 2048)), per_group = 4 * per_wave;

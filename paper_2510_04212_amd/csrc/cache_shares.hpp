@@ -134,7 +134,7 @@ struct CacheForm {
   size_t slot_floats(int d) const { return (size_t)(4 / KW) * RT * (d / 16 * 256 + 32); }
   bool many_parts;                         // few segments for the shares: each is in many parts
   // notes, then slots
-  size_t workspace_bytes(int d) const { return split && shares > 1 ? shares * sizeof(Join) + 2 * (size_t)shares * slot_floats(d) * sizeof(float) : 0; }
+  size_t workspace_bytes(int d) const { return split ? shares * sizeof(Join) + 2 * (size_t)shares * slot_floats(d) * sizeof(float) : 0; }
 };
 // No share is smaller.  Four waves that share the blocks out: one block; sharing them: two (20 rows of 4 sequences of 1000 tokens, H 32/8, d 128: 24.7 us
 // at eight blocks, 21.5 at four, 19.7 at two; 64 rows of 32768: 33.3, 28.7, 29.6; 8400 rows of 2100: 70.8, 73.6, 73.9).
