@@ -267,13 +267,14 @@ DEVI void take_out_nan(Acc<D, RT>& a, VCodes<D>& v, const int (&limit)[RT], int 
 // The maximum that probabilities are taken relative to is let fall behind the true one by up to kSlack (a factor of 2^kSlack, harmless in float32 and
 // bf16 alike), so that the accumulators are hardly ever rescaled.
 //
-// Two tiles of rows: of the two waves that share a SIMD, the one that multiplies goes first, so that the other's softmax fills in (2048 queries over
-// 16384 tokens 632 -> 600 us; d = 64, 4096 queries of 4 sequences 463 -> 422; with one wave a SIMD, d = 256, 243 -> 248, not there).
+// Of the two waves that share a SIMD, the one that multiplies goes first, so that the other's softmax fills in (2048 queries over 16384 tokens, H 32/8,
+// d 128: 632 -> 600 us; 16 queries of 64 sequences of 4300: 128 -> 120; d = 64, 4096 queries of 4 sequences: 463 -> 422; with one wave a SIMD, d = 256: 243 ->
+// 248, not there).
 constexpr float kSlack = 8.f;
 template <int D, int RT, class F>
 DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, float scale_log2,
                      const int (&limit)[RT], bool masked, int t0, int g, F&& after_scores) {
-  constexpr bool kMultipliesFirst = RT == 2 && D < 256;
+  constexpr bool kMultipliesFirst = D < 256;
   f32x4 s[RT][4];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
