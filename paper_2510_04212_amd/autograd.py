@@ -126,5 +126,8 @@ def _aligned(t):
 def rope(q, k=None, frequencies=None, positions=None, interleaved=False, magnitude=1.0):
     """(q, k) with the first 2 * len(frequencies) columns rotated by their positions, differentiable in q and k; k may be absent (None
     comes back).  frequencies, magnitude: binding.rope_frequencies(...); positions: int32 [N] or [B,N], by default 0 .. N-1.  Results are laid
-    out like q and k (any strides with a contiguous last dimension), ready for attention()."""
+    out like q and k (any strides with a contiguous last dimension), ready for attention().
+
+    Capturing the backward pass into a graph: drop the results of earlier eager passes through the same leaves first (torch ties a leaf's
+    gradient to the stream of the pass that is alive)."""
     return _Rope.apply(q, k, frequencies, positions, bool(interleaved), float(magnitude), False)

@@ -513,12 +513,19 @@ def _on(device, stream, make):
         return make()
 
 
-def _rows(t, name, device=None):
+def _fit(*sizes):
+    """Checks sizes that the C ABI takes as int (ctypes would cut them)."""
+    if any(not -2 ** 31 <= s < 2 ** 31 for s in sizes):
+        raise ValueError(f"sizes must be below 2^31: {sizes}")
+
+
+def _rows(t, name):
     """Checks a CUDA bfloat16 tensor [B,H,N,d] on the current GPU with a contiguous last dimension; any other strides."""
     if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
         raise ValueError(f"{name} must be a CUDA bfloat16 tensor [B,H,N,d] whose last dimension is contiguous")
     if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current GPU")
+    _fit(*t.shape)
     return t.shape
 
 
@@ -570,6 +577,7 @@ def attn_rope(Q, K=None, frequencies=None, positions=None, interleaved=False, ma
     if frequencies is None or frequencies.dim() != 1:
         raise ValueError("frequencies must be a float64 tensor [rot/2]")
     _dense(frequencies, "frequencies", frequencies.shape, torch.float64, device)
+    _fit(2 * frequencies.shape[0])
     positions_stride = 0
     if positions is not None:
         if positions.dim() not in (1, 2) or positions.shape[-1] != N or (positions.dim() == 2 and positions.shape[0] != B) \
@@ -614,6 +622,7 @@ def _cache_shape(cache, name="cache"):
     device = cache.K.device
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current GPU")
+    _fit(capacity)
     nb = capacity // CACHE_BLOCK
     _dense(cache.K, name + ".K", (B, H_kv, nb * CACHE_BLOCK, d), torch.float8_e4m3fn, device)
     _dense(cache.V, name + ".V", (B, H_kv, nb, d, CACHE_BLOCK), torch.float8_e4m3fn, device)
@@ -645,6 +654,7 @@ def attn_cache_append(cache, K, V, lengths, counts=None, stream=None):
 
 def cache_fwd_workspace_bytes(B, H, H_kv, N, d, capacity):
     """Workspace that attn_cache_fwd needs for this problem (0: none)."""
+    _fit(B, H, H_kv, N, d, capacity)
     return int(_lib.attn_cache_fwd_workspace_bytes(B, H, H_kv, N, d, capacity))
 
 
@@ -730,6 +740,7 @@ def attn_cache_evict(cache, weights, lengths, budget, recent, out=None, stream=N
     _sequence_lengths(lengths, None, B, device)
     if budget < 1:
         raise ValueError("budget must be positive")
+    _fit(budget, recent)
     if out is None:
         out = _on(device, stream, lambda: cache_empty(B, H_kv, -(-budget // CACHE_BLOCK) * CACHE_BLOCK, d, device))
     Bo, Ho, capacity_out, do, device_out = _cache_shape(out, "out")

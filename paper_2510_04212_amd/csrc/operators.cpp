@@ -12,6 +12,8 @@
 #include <ATen/ATen.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <c10/hip/HIPFunctions.h>
+#include <algorithm>
+#include <climits>
 #include <optional>
 #include <tuple>
 #include <vector>
@@ -34,8 +36,8 @@ bool rows(const Tensor& t, Device device) {
   if (!on(t, device, at::kBFloat16) || t.dim() != 4 || t.numel() == 0 || t.stride(3) != 1) return false;
   if (reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 != 0) return false;
   for (int i = 0; i < 3; ++i)
-    if (t.stride(i) < 0 || t.stride(i) % 8 != 0) return false;
-  return true;
+    if (t.stride(i) < 0 || t.stride(i) % 8 != 0 || t.size(i) > INT_MAX) return false;
+  return t.size(3) <= INT_MAX;
 }
 bool dense(const Tensor& t, Device device, at::ScalarType type, at::IntArrayRef shape) {
   return on(t, device, type) && t.sizes() == shape && t.is_contiguous();
@@ -57,7 +59,7 @@ struct Cache {
     if (!on(K, device, at::kFloat8_e4m3fn) || K.dim() != 4 || K.numel() == 0) return false;
     B = K.size(0); H = K.size(1); capacity = K.size(2); d = K.size(3);
     const int64_t nb = capacity / ATTN_CACHE_BLOCK;
-    return capacity % ATTN_CACHE_BLOCK == 0 && dense16(K, device, at::kFloat8_e4m3fn, {B, H, capacity, d}) &&
+    return std::max(std::max(B, H), std::max(capacity, d)) <= INT_MAX && capacity % ATTN_CACHE_BLOCK == 0 && dense16(K, device, at::kFloat8_e4m3fn, {B, H, capacity, d}) &&
            dense16(V, device, at::kFloat8_e4m3fn, {B, H, nb, d, ATTN_CACHE_BLOCK}) && dense16(K_scale, device, at::kFloat, {B, H, nb}) &&
            dense16(V_scale, device, at::kFloat, {B, H, nb});
   }
@@ -78,7 +80,7 @@ std::optional<std::tuple<Tensor, OptTensor>> rope(const Tensor& q, const OptTens
   if (!rows(q, device) || (k && !rows(*k, device))) return std::nullopt;
   const int64_t B = q.size(0), H = q.size(1), N = q.size(2), d = q.size(3);
   if (k && (k->size(0) != B || k->size(2) != N || k->size(3) != d)) return std::nullopt;
-  if (!on(frequencies, device, at::kDouble) || frequencies.dim() != 1 || !frequencies.is_contiguous()) return std::nullopt;
+  if (!on(frequencies, device, at::kDouble) || frequencies.dim() != 1 || !frequencies.is_contiguous() || 2 * frequencies.numel() > d) return std::nullopt;
   long long stride = 0;
   if (positions) {
     const Tensor& p = *positions;

@@ -242,6 +242,40 @@ def test_chunks(lib, d, causal, cap):
         _run(q, c, lengths, counts, 1.5 * d ** -0.5, causal, f"N {N}", w_in)
 
 
+@pytest.mark.parametrize("d", DIMS)
+@pytest.mark.parametrize("causal", (True, False))
+def test_many_rows(lib, d, causal):
+    """More rows than 3 d at any head size, and an odd number of blocks."""
+    N, group, cap, lengths, counts = 210, 4, 448, [448, 215, 130], [210, 200, 130]
+    g = _gen(d)
+    c = _filled(g, 3, 2, cap, d, lengths)
+    w_in = torch.rand((3, 2, cap), generator=g).to(DEV)
+    _run(_bf16(g, 3, 2 * group, N, d).to(DEV), c, lengths, counts, d ** -0.5, causal, w_in=w_in)
+
+
+@pytest.mark.parametrize("N,cap", [(1, 2112), (20, 1088)])
+def test_a_work_group_for_each_of_many_segments(lib, N, cap):
+    """Segments that fill the chip by themselves are not shared out up to twice the length."""
+    B, Hkv, d = 33, 16, 32
+    g = _gen(N)
+    lengths = [cap if b % 4 == 0 else (b * 977) % cap for b in range(B)]
+    c = _filled(g, B, Hkv, cap, d, lengths)
+    assert binding.cache_fwd_workspace_bytes(B, Hkv, Hkv, N, d, cap) == 0 < binding.cache_fwd_workspace_bytes(B, Hkv, Hkv, N, d, 4 * cap)
+    _run(_bf16(g, B, Hkv, N, d).to(DEV), c, lengths, [min(N, l) for l in lengths], d ** -0.5, True)
+
+
+def test_sizes_beyond_int_are_refused(lib):
+    """Views of any size cost no memory."""
+    x = torch.ones(64, dtype=torch.bfloat16, device=DEV).expand(1, 1, 2 ** 31, 64)
+    c, out = binding.cache_empty(1, 1, 64, 64, DEV), binding.cache_empty(1, 1, 64, 64, DEV)
+    f, _ = binding.rope_frequencies(64, device=DEV)
+    weights = torch.zeros(1, 1, 64, device=DEV)
+    for call in (lambda: binding.attn_rope(x, None, f), lambda: binding.attn_cache_append(c, x, x, _i32([64])), lambda: binding.attn_cache_fwd(x, c, _i32([64]), 0.1),
+                 lambda: binding.attn_cache_evict(c, weights, _i32([0]), 2 ** 32 + 64, 0, out=out), lambda: binding.cache_fwd_workspace_bytes(1, 1, 1, 1, 64, 2 ** 32 + 64)):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_more_queries_than_tokens(lib):
     """The first queries of a chunk that is longer than its cache see nothing."""
     g = _gen(11)

@@ -147,3 +147,30 @@ def test_other_streams_and_graphs(lib):
         eager = lib.attn_rope(x, k, f, positions=at)
         torch.cuda.synchronize()
         assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
+
+
+def test_a_captured_backward(lib):
+    q, k = _draw(14, 1, 4, 33, 64).requires_grad_(), _draw(15, 1, 2, 33, 64).requires_grad_()
+    f, _ = lib.rope_frequencies(64, device=DEV)
+    gq, gk = _draw(16, 1, 4, 33, 64), _draw(17, 1, 2, 33, 64)
+
+    def step():                            # nothing of the pass outlives it
+        a, b = autograd.rope(q, k, f)
+        return (a.detach(), b.detach(), *torch.autograd.grad((a, b), (q, k), (gq, gk)))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for times in (1, 2, -3):
+        with torch.no_grad():
+            q.mul_(times)
+            gk.mul_(times)
+        graph.replay()
+        eager = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, eager))
