@@ -349,7 +349,8 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
 
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
 //
-// KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead.  KW = 1, many rows: bound by
+// KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead (one token of 64 sequences of 4300, H 32/8, d
+// 128: 103 us, 5.5 TB/s).  KW = 1, many rows: bound by
 // the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers a block ahead (three blocks ahead, in four
 // buffers: 16 queries of 64 sequences of 4300 tokens, H 32/8, d 128, 139 us; one ahead, in two: 125.  2048 queries over 16384: 636 and 620).
 template <int D, int RT, int KW, bool SPLIT>
@@ -662,7 +663,7 @@ template <int D> hipError_t launch_fwd(const AttendArgs& p, hipStream_t stream) 
 //
 // Few row tiles: bound by K's bytes; a wave takes up to 8 blocks one after the other, the next one's codes on their way (one token of 32
 // sequences of 2000 to 4160 tokens, H 32/8, d 128: 25 us with a block per wave, 22.6 with 2, 21.4 with 8).  Many: by the exponentials and the products, and by what a row
-// tile costs besides (addresses, loads), which two blocks share (500 queries, H 32/8, over 16384 tokens: 157 us with one block, 102 with two);
+// tile costs besides (addresses, loads), which two blocks share (500 queries, H 32/8, over 16384 tokens: 156 us with one block, 95 with two);
 // the four waves of a work-group take the row tiles in turn.
 DEVI float sum_over_16_lanes(float x) {        // the same in all 16: four rotations of the row
   x += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, false));
@@ -871,8 +872,8 @@ template <int D> hipError_t launch_weights(const WeighArgs& p, hipStream_t strea
   const unsigned nb = (unsigned)(p.cache.capacity / kBlock);
   constexpr int NB = D <= 128 ? 2 : 1;       // (a lane's registers hold one block's keys of d = 256)
   // The crossing point is where the second block's widened keys are paid for, later the more there are of them.  us, few / many, 32 sequences of 4096
-  // (d = 128; 16 of d = 32, 64; 8 of d = 256): 96 rows 75 / 119, 256 148 / 164, 384 204 / 211, 512 264 / 255, 1024 513 / 387; d = 32: 96 rows 19.2 / 19.7, 128
-  // 23.4 / 21.7; d = 64: 128 27 / 30, 192 37.4 / 37.7, 256 47 / 44; d = 256: 64 32 / 54, 512 132 / 152.
+  // (d = 128; 16 of d = 32, 64; 8 of d = 256): 96 rows 76 / 119, 256 151 / 167, 384 210 / 204, 512 264 / 250, 1024 516 / 375; d = 32: 96 rows 19.2 / 20.8, 128
+  // 23.4 / 22.4; d = 64: 128 27 / 30, 192 37.4 / 36.7, 256 47 / 42; d = 256: 96 38 / 59, 512 132 / 151.
   if ((long long)p.N * p.group <= 3 * D) {
     // a block per wave until the waves are two to a SIMD, then more, up to 8
     const long long blocks = (long long)p.B * p.H_kv * nb;

