@@ -397,10 +397,10 @@ int attn_cache_append(const void* K, const void* V, const long long* strides, vo
  *   workspace  attn_cache_fwd_workspace_bytes(...) bytes, 16-byte aligned; contents on entry are ignored; free for reuse once the stream has
  *            passed the call.  Where that is 0 it may be NULL.  Calls that can overlap in time need one each.
  * A query that sees nothing, and queries i >= counts[b], give O = 0 and LSE = -infinity.  Scores, statistics and sums are float32, the row
- * sum that of the float32 probabilities; these are rounded to bf16 as the operand of the product with V, and O is rounded once.  A NaN among the values of a token does not reach the queries that do not see it.  Deterministic; which float32 sums
- * are formed in which order depends on the whole batch's lengths, as key blocks are shared out evenly over the chip.
+ * sum that of the float32 probabilities; these are rounded to bf16 as the operand of the product with V, and O is rounded once.  A NaN among the values of a
+ * token does not reach the queries that do not see it.  Deterministic; which float32 sums are formed in which order depends on the whole batch's lengths, as key blocks are shared out evenly over the chip.
  * ATTN_ERR_UNSUPPORTED, for attn_cache_weights as well, where B * H_kv * T * (capacity / 64 + 5) >= 2^30 (seconds of work), T the number of
- * tiles of 16, 32 or 128 that R = N H / H_kv rows make (R <= 16, <= 32, more).
+ * tiles of 16, 64 or 128 that R = N H / H_kv rows make (R <= 16, <= 64, more).
  */
 size_t attn_cache_fwd_workspace_bytes(int B, int H, int H_kv, int N, int d, int capacity);
 int attn_cache_fwd(const void* Q, const long long* strides, const void* K_cache, const void* V_cache,

@@ -280,10 +280,12 @@ template <int ROOM> __global__ __launch_bounds__(kSelectThreads) void attn_cache
 
 // ---- evict, second kernel: one work-group per block of the new cache.  Its scales are the largest of its tokens' old ones, so that
 // codes are only ever multiplied by powers of two <= 1.  V's blocks hold columns: of each, four tokens' codes are picked from 8 bytes where the four
-// lie so near each other (nearly all do while most tokens stay), and one by one elsewhere.  Bound by bytes: 4096 of 4400 tokens of 128 heads, d 128: 72 us,
-// 3.8 TB/s.
+// lie so near each other (nearly all do while most tokens stay), and one by one elsewhere.  Bound by bytes: 4096 of 4400 tokens of 128 heads, d 128: 70 us,
+// 3.9 TB/s.
 //
-// Two loads one after the other, the kept positions and what they lead to: all of a thread's codes are on their way before anything waits.
+// Two loads one after the other, the kept positions and what they lead to: all of a thread's codes are on their way before anything waits.  The old K is
+// read once and past the caches (the whole call 86.1 -> 83.4 us, with a token's attention behind it 119.4 -> 116.7); not V, whose lines neighbouring blocks share (100), nor
+// what is written, which attention reads next (4 sequences of 8192: 50.5 -> 53 with it, though 512 heads, 0.5 GB, gain 8 %).
 template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_gather_kernel(EvictArgs p) {
   const int b = blockIdx.z, h = blockIdx.y, j = blockIdx.x, tid = threadIdx.x;
   const size_t bh = (size_t)b * p.H_kv + h;
@@ -305,7 +307,7 @@ template <int D> __global__ __launch_bounds__(kThreads) void attn_cache_gather_k
 #pragma unroll
   for (int k = 0; k < NK; ++k) {
     xk[k] = u32x4{0, 0, 0, 0};
-    if (from_k[k] >= 0) xk[k] = *reinterpret_cast<const u32x4*>(K + (size_t)from_k[k] * D + (tid + k * kThreads) % CH * 16);
+    if (from_k[k] >= 0) xk[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(K + (size_t)from_k[k] * D + (tid + k * kThreads) % CH * 16));
   }
   const int first = max(from_v[0], 0), window = min(first % kBlock & ~3, kBlock - 8);       // of the source block's tokens: 8 from here
   unsigned pick = 0;                       // of those, v_perm's selector: 12 is a zero
