@@ -280,8 +280,8 @@ template <int ROOM> __global__ __launch_bounds__(kSelectThreads) void attn_cache
 
 // ---- evict, second kernel: one work-group per block of the new cache.  Its scales are the largest of its tokens' old ones, so that
 // codes are only ever multiplied by powers of two <= 1.  V's blocks hold columns: of each, four tokens' codes are picked from 8 bytes where the four
-// lie so near each other (nearly all do while most tokens stay), and one by one elsewhere.  Bound by bytes: 4096 of 4400 tokens of 128 heads, d 128: 70 us,
-// 3.9 TB/s.
+// lie so near each other (nearly all do while most tokens stay), and one by one elsewhere.  Bound by bytes: 4096 of 4400 tokens of 128 heads, d 128: 71 us,
+// 3.8 TB/s.
 //
 // Two loads one after the other, the kept positions and what they lead to: all of a thread's codes are on their way before anything waits.  The old K is
 // read once and past the caches (the whole call 86.1 -> 83.4 us, with a token's attention behind it 119.4 -> 116.7); not V, whose lines neighbouring blocks share (100), nor

@@ -147,11 +147,14 @@ inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
 // them (32 rows of 64 x 4300: 132 us with blocks of a wave's own, 118 shared; 64 rows: 164 and 123).  From 65 on two row tiles a wave (68 rows:
 // 284 us with one, 169 with two; 128 rows: 274 and 184).
 //
-// Split.  Sharing out costs 5 to 8 us (finding the segment, the second kernel) and pays where a segment is long for the work-groups that there are: beyond
-// 16 blocks, 32 where there is a segment for every work-group that runs at once, as they then fill the chip by themselves; for up to 16 rows, whose
-// blocks four waves share out, 32 from a sixteenth of that on, and 64.  Whole / split, us, full caches, H 32/8, d 128: one token, capacity 1024:
-// 1 sequence 8.8 / 14.8, 64 25.7 / 30.3; 2048: 1 15.6 / 14.5, 16 15.3 / 22.7; 4096: 1 25.0 / 13.3, 4 23 / 17, 64 91 / 98, and 60 / 66 at lengths of
-// 256 to 4096.  64 rows: 1024: 1 19 / 23; 2048: 4 33 / 24, 64 59 / 63; 4096: 4 61 / 28.  2048 queries of 2048 tokens 65 / 71, 4096 of 4096 197 / 175.
+// Split.  Sharing out costs 5 to 10 us (finding the segment, the second kernel) and pays where the longest segment alone takes longer than all bytes
+// together, that is for few segments, long ones, and lengths far apart.  Whole / split, us, H 32/8:
+//   up to 16 rows, a segment's length counted in blocks of 16 KB of d = 128: from 16 (few segments) over 28 to 64, the more segments there are.
+//     d = 128, one token, capacity 1024: 1 sequence 8.8 / 14.8;  2048: 1 15.6 / 14.5, 16 15.3 / 22.7;  2112: 6 15.5 / 16.6, 24 20.7 / 30.5;  3008: 6 19.6 / 18.1,
+//     12 19.8 / 24.7;  4096: 1 25.0 / 13.3, 12 28.9 / 30.5 (25.4 / 22.2 at lengths of 256 to 4096), 24 36.8 / 48.4 (30.4 / 32.0), 64 91 / 98 (60 / 66);
+//     8192: 32 91 / 115 full, 61 / 61 ragged, 51 / 35 with one sequence in eight full.  d = 64, 4096: 4 12.1 / 15.3, 24 16.9 / 24.2
+//   more rows, shared blocks: 16, 32 where there is a segment for every work-group that runs at once.  64 rows: 1024: 1 19 / 23;  2048: 4 33 / 24, 64 59 / 63;
+//     4096: 4 61 / 28.  2048 queries of 2048 tokens 65 / 71, 4096 of 4096 197 / 175.
 inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
   const long long rows = (long long)N * (H / H_kv);
   CacheForm f;
@@ -161,9 +164,13 @@ inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) 
   const double most_shares = cache_units(B, H_kv, f, capacity) / (f.KW == 4 ? kLeastUnits<4> : kLeastUnits<1>);
   const int most = d == 256 ? 256 : 512;   // as many as run at once
   const double segments = (double)B * H_kv * f.tiles;
-  int whole = segments >= most ? 32 : 16;
-  if (f.KW == 4 && segments >= most / 16) whole = segments >= most ? 64 : 32;
-  f.split = capacity / kBlock > whole || f.tiles > 65535;       // (the grid's second dimension)
+  const int nb = capacity / kBlock;
+  bool whole = nb <= (f.KW == 1 && segments >= most ? 32 : 16);
+  if (f.KW == 4 && segments >= most / 16) {
+    const double limit = 28 + 102 * segments / most;
+    whole = nb <= 64 && nb * (d / 128.0) <= (limit < 64 ? limit : 64);
+  }
+  f.split = !whole || f.tiles > 65535;     // (the grid's second dimension)
   f.shares = most_shares >= most ? most : most_shares < 1 ? 1 : (int)most_shares;
   f.many_parts = f.shares > 4 * segments;
   return f;
