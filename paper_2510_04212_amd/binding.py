@@ -641,7 +641,8 @@ def attn_cache_append(cache, K, V, lengths, counts=None, stream=None):
     """Quantises the new tokens K, V [B,H_kv,N,d] (any strides) into the cache, in place.
 
     lengths: int32 [B], the tokens of each sequence in its cache, the new ones among them; counts: int32 [B], how many of the N tokens (the
-    first ones) a sequence really has; all where absent."""
+    first ones) a sequence really has; all where absent.  Tokens at positions past the capacity are not stored (lengths are on the device, and
+    nothing is reported)."""
     if stream is None and _operators.cache_append(*cache, K, V, lengths, counts):
         return
     B, H_kv, capacity, d, device = _cache_shape(cache)
@@ -728,9 +729,10 @@ def attn_cache_evict(cache, weights, lengths, budget, recent, out=None, stream=N
     """(out, weights_out, kept): the cache cut down to min(lengths, budget) tokens of each sequence and head, the last `recent` and, of those
     before, the ones with the largest weights (equal ones: the earliest), in their order.
 
-    weights: float32 [B,H_kv,capacity] of attn_cache_weights.  out: another Cache with room for `budget` tokens; a new one of the least
-    capacity when absent.  weights_out: float32 [B,H_kv,capacity of out], the kept tokens' weights, then 0.  kept: int32
-    [B,H_kv,budget], their old positions, then -1.  The caller's lengths are then lengths.clamp(max=budget)."""
+    weights: float32 [B,H_kv,capacity] of attn_cache_weights.  out: another Cache with room for `budget` tokens and for those that are
+    to follow (one that is full takes no more); a new one of the old capacity when absent (of the budget, if that is larger).
+    weights_out: float32 [B,H_kv,capacity of out], the kept tokens' weights, then 0.  kept: int32 [B,H_kv,budget], their old positions,
+    then -1.  The caller's lengths are then lengths.clamp(max=budget); positions for attn_rope go on counting from the old lengths."""
     if stream is None and out is not None:
         result = _operators.cache_evict(*cache, weights, lengths, *out, budget, recent)
         if result is not None:
@@ -742,7 +744,7 @@ def attn_cache_evict(cache, weights, lengths, budget, recent, out=None, stream=N
         raise ValueError("budget must be positive")
     _fit(budget, recent)
     if out is None:
-        out = _on(device, stream, lambda: cache_empty(B, H_kv, -(-budget // CACHE_BLOCK) * CACHE_BLOCK, d, device))
+        out = _on(device, stream, lambda: cache_empty(B, H_kv, max(capacity, -(-budget // CACHE_BLOCK) * CACHE_BLOCK), d, device))
     Bo, Ho, capacity_out, do, device_out = _cache_shape(out, "out")
     if (Bo, Ho, do, device_out) != (B, H_kv, d, device):
         raise ValueError("out must have the sequences, heads and head size of the cache")

@@ -621,3 +621,28 @@ def test_training_with_positions(lib):
     for got, w in [(o, want)] + [(x.grad, y.grad) for x, y in zip(leaves, ref)]:
         w, got = w.detach(), got.detach().double().cpu()
         assert (got - w).norm() <= 2e-2 * w.norm() and (got - w).abs().max() <= 5e-2 * max(1.0, w.abs().max().item())
+
+
+def test_answering_goes_on_after_an_eviction(lib):
+    """The cache that attn_cache_evict makes by itself has room for the tokens that follow."""
+    g = _gen(51)
+    B, H, Hkv, d, cap, budget = 2, 4, 2, 64, 256, 128
+    lengths = [250, 90]
+    c = _filled(g, B, Hkv, cap, d, lengths)
+    w = torch.rand((B, Hkv, cap), generator=g).to(DEV)
+    c, w, _ = _check_evict(c, w, lengths, budget, 16)
+    assert c.K.shape[2] == cap and w.shape == (B, Hkv, cap)
+    lengths = [min(n, budget) for n in lengths]
+    for _ in range(3):
+        lengths = [n + 1 for n in lengths]
+        q, k, v = (_bf16(g, B, h, 1, d) for h in (H, Hkv, Hkv))
+        binding.attn_cache_append(c, k.to(DEV), v.to(DEV), _i32(lengths))
+        (K, V), (ek, ev) = _dequantised(c), _values(c)[1]
+        for b, n in enumerate(lengths):                    # an E4M3 code: half a step, 2^-4 of the value or 2^-10 of the scale
+            for x, got, e in ((k, K, ek), (v, V, ev)):
+                want = x[b, :, 0].double().numpy()
+                assert (np.abs(got[b, :, n - 1] - want) <= 2.0 ** -4 * np.abs(want) + 2.0 ** (e[b, :, (n - 1) // 64, None] - 10)).all()
+        _, _, w = _run(q.to(DEV), c, lengths, None, d ** -0.5, True, w_in=w)
+    # a budget beyond the old cache's capacity has its room
+    more, w2, _ = binding.attn_cache_evict(c, w, _i32(lengths), 300, 0)
+    assert more.K.shape[2] == 320 and w2.shape == (B, Hkv, 320)
