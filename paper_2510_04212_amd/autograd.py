@@ -120,7 +120,7 @@ class _Rope(torch.autograd.Function):
 def _aligned(t):
     """A gradient in a layout that attn_rope takes (sum().backward() brings an expanded scalar)."""
     fits = t.stride(3) == 1 and all(s % 8 == 0 for s in t.stride()[:3]) and t.data_ptr() % 16 == 0
-    return t if fits else t.contiguous()
+    return t if fits else t.clone(memory_format=torch.contiguous_format)          # (contiguous() keeps one that begins off 16 bytes)
 
 
 def rope(q, k=None, frequencies=None, positions=None, interleaved=False, magnitude=1.0):

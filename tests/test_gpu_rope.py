@@ -174,3 +174,17 @@ def test_a_captured_backward(lib):
         eager = step()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(out, eager))
+
+
+def test_a_gradient_that_begins_off_16_bytes(lib):
+    """cat's backward hands out views that begin anywhere."""
+    q, k = _draw(19, 1, 2, 9, 64).requires_grad_(), _draw(20, 1, 2, 9, 64).requires_grad_()
+    f, _ = lib.rope_frequencies(64, device=DEV)
+    a, b = autograd.rope(q, k, f)
+    odd = torch.zeros(3, dtype=torch.bfloat16, device=DEV)
+    out = torch.cat((odd, a.flatten(), odd, b.flatten()))
+    g = _draw(21, out.numel())
+    dq, dk = torch.autograd.grad(out, (q, k), g)
+    n = q.numel()
+    want = lib.attn_rope(g[3:3 + n].clone().view_as(q), g[6 + n:].clone().view_as(k), f, inverse=True)
+    assert torch.equal(dq, want[0]) and torch.equal(dk, want[1])
