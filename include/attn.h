@@ -329,7 +329,7 @@ int attn_fwd_ws(const void* Q, const void* K, const void* V, void* O, float* LSE
  * Rotary positions: the first `rot` columns (even, 2 <= rot <= d) of every row of Q [B,H,N,d] and K [B,H_kv,N,d] are rot/2 pairs, and
  * pair i of the token at position p becomes  magnitude * (x cos - y sin, x sin + y cos)  of the angle p * frequencies[i];
  * columns from rot on are copied.  Products in float32, rounded to bf16 once; angles in float64.
- *   K, K_out         may both be NULL (H_kv is then ignored): Q alone.  H_kv need not divide H.
+ *   K, K_out         may both be NULL (H_kv is then ignored): Q alone.  H_kv need not divide H; with H == 0 the keys are rotated alone.
  *   Q_out, K_out     may be Q and K themselves (with the same strides); they must not overlap otherwise
  *   strides          12 numbers on the HOST, or NULL (all contiguous): stride_b, stride_h, stride_n of Q, K, Q_out, K_out in elements.
  *                    Multiples of 8; inputs >= 0 (0: an expanded dimension), outputs > 0.

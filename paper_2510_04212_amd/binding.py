@@ -591,7 +591,7 @@ def attn_rope(Q, K=None, frequencies=None, positions=None, interleaved=False, ma
     for t, like, n in ((Q_out, Q, "Q_out"), (K_out, K, "K_out")):
         if (t is None) != (like is None) or (t is not None and _rows(t, n) != like.shape):
             raise ValueError(f"{n} must have the shape of {n[0]}")
-    if B and H:
+    if B and H + H_kv:
         _check(_lib.attn_rope(_ptr(Q), _ptr_or_none(K), _ptr(Q_out), _ptr_or_none(K_out), _strides(Q, K, Q_out, K_out),
                               _ptr_or_none(positions), positions_stride, _ptr(frequencies), B, H, H_kv, N, d, 2 * frequencies.shape[0],
                               int(bool(interleaved)), float(magnitude), int(bool(inverse)), _stream(stream)))

@@ -55,6 +55,15 @@ extern "C" int attn_rope(const void* Q, const void* K, void* Q_out, void* K_out,
   if (H_kv < 0 || rot < 0) return ATTN_ERR_BAD_ARG;
   if ((K == nullptr) != (K_out == nullptr)) return ATTN_ERR_NULL;
   if (!K) H_kv = 0;
+  if (H == 0 && H_kv > 0) {                // no queries here: the keys alone
+    long long of_keys[12] = {};
+    if (strides) {
+      std::copy_n(strides + 3, 3, of_keys);
+      std::copy_n(strides + 9, 3, of_keys + 6);
+    }
+    return attn_rope(K, nullptr, K_out, nullptr, strides ? of_keys : nullptr, positions, positions_stride_b, frequencies, B, H_kv, 0, N, d, rot,
+                     interleaved, magnitude, inverse, stream);
+  }
   int st = check_rows(B, H, N, d, &empty);
   if (st != ATTN_OK) return st;
   if (empty) return ATTN_OK;

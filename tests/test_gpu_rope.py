@@ -188,3 +188,16 @@ def test_a_gradient_that_begins_off_16_bytes(lib):
     n = q.numel()
     want = lib.attn_rope(g[3:3 + n].clone().view_as(q), g[6 + n:].clone().view_as(k), f, inverse=True)
     assert torch.equal(dq, want[0]) and torch.equal(dk, want[1])
+
+
+def test_keys_without_queries(lib):
+    """A rank may have key heads alone: they are rotated all the same."""
+    k = _draw(18, 2, 3, 21, 64)
+    q = torch.empty(2, 0, 21, 64, dtype=torch.bfloat16, device=DEV)
+    f, _ = lib.rope_frequencies(64, device=DEV)
+    want, _ = lib.attn_rope(k, None, f)
+    for keys in (k, k.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)):
+        a, b = lib.attn_rope(q, keys, f)
+        assert a.shape == q.shape and torch.equal(b, want)
+    lib.attn_rope(q, k, f, Q_out=q, K_out=k)
+    assert torch.equal(k, want)

@@ -144,3 +144,16 @@ def test_binding_refuses_tensors_that_are_not_the_gpus(binding):
                  lambda: binding.attn_cache_fwd(cpu, cache, lengths, 0.1), lambda: binding.attn_cache_evict(cache, lengths, lengths, 10, 1)):
         with pytest.raises((ValueError, RuntimeError)):
             call()
+
+
+def test_rope_of_keys_alone_is_checked_like_any(binding):
+    lib = binding.raw()
+
+    def rope(K=_p(2), Ko=_p(4), strides=None, f=_p(5), B=1, Hkv=2, N=8, d=64, rot=64):
+        return lib.attn_rope(None, K, None, Ko, strides, None, 0, f, B, 0, Hkv, N, d, rot, 0, 1.0, 0, None)
+
+    assert rope(B=0) == OK and rope(Hkv=0) == OK
+    assert rope(K=MIS) == BAD and rope(f=None) == NULL and rope(Ko=None) == NULL and rope(rot=3) == BAD and rope(d=80, rot=16) == UNSUP
+    good, other = (1024, 512, 64), (4096, 2048, 64)
+    assert rope(strides=_strides(*good, 1024, 512, 60, *good, *good)) == BAD and rope(strides=_strides(*good, *good, *good, 1024, 0, 64)) == BAD
+    assert rope(Ko=_p(2), strides=_strides(*good, *good, *good, *other)) == BAD          # in place with other strides
