@@ -712,6 +712,8 @@ def attn_cache_weights(Q, cache, LSE, lengths, softmax_scale, causal=True, count
         if result is not None:
             return result if out is None else out
     B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
+    if H == 0 and B and H_kv:              # (the library does nothing then, and out would stay as it is)
+        raise ValueError("Q must have heads")
     _sequence_lengths(lengths, counts, B, device)
     _dense(LSE, "LSE", (B, H, N), torch.float32, device)
     shape = (B, H_kv, capacity)

@@ -646,3 +646,10 @@ def test_answering_goes_on_after_an_eviction(lib):
     # a budget beyond the old cache's capacity has its room
     more, w2, _ = binding.attn_cache_evict(c, w, _i32(lengths), 300, 0)
     assert more.K.shape[2] == 320 and w2.shape == (B, Hkv, 320)
+
+
+def test_weights_of_no_queries_are_refused(lib):
+    c = binding.cache_empty(2, 3, 64, 64, DEV)
+    q = torch.empty(2, 0, 5, 64, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError):
+        binding.attn_cache_weights(q, c, torch.empty(2, 0, 5, device=DEV), _i32([5, 9]), 0.125)
