@@ -553,7 +553,12 @@ def _strides(*tensors):
 
 
 def _ptr_or_none(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    """NULL for an absent argument.  A tensor subclass that has its data elsewhere has that address, too: it is not absent."""
+    if t is None:
+        return None
+    if t.data_ptr() == 0 and t.numel() > 0:
+        raise ValueError(f"a {type(t).__name__} without memory of its own cannot be passed on")
+    return ctypes.c_void_p(t.data_ptr())
 
 
 def attn_rope(Q, K=None, frequencies=None, positions=None, interleaved=False, magnitude=1.0, inverse=False, Q_out=None, K_out=None,

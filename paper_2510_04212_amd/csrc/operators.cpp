@@ -27,9 +27,10 @@ using Device = c10::DeviceIndex;
 
 void* stream_of(Device device) { return static_cast<void*>(c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(device).stream()); }
 
+// (A tensor subclass that has its data elsewhere has the address NULL, which the library would take for an argument that is not there.)
 bool on(const Tensor& t, Device device, at::ScalarType type) {
   return t.defined() && t.is_cuda() && t.layout() == at::kStrided && t.scalar_type() == type && t.get_device() == device && !t.is_neg() &&
-         !t.is_conj();
+         !t.is_conj() && t.data_ptr() != nullptr;
 }
 // bf16 rows [B,H,N,d] the library takes as they are; least: of a stride
 bool rows(const Tensor& t, Device device) {

@@ -201,3 +201,32 @@ def test_keys_without_queries(lib):
         assert a.shape == q.shape and torch.equal(b, want)
     lib.attn_rope(q, k, f, Q_out=q, K_out=k)
     assert torch.equal(k, want)
+
+
+class _NoMemory(torch.Tensor):
+    """A tensor subclass whose data lie elsewhere, as of distributed tensors."""
+    @staticmethod
+    def __new__(cls, t):
+        return torch.Tensor._make_wrapper_subclass(cls, t.shape, dtype=t.dtype, device=t.device)
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise NotImplementedError(str(func))
+
+
+def test_optional_tensors_without_memory_are_refused(lib):
+    """Their address is NULL, which the library takes for an absent argument."""
+    q = _draw(22, 2, 2, 9, 64)
+    f, _ = lib.rope_frequencies(64, device=DEV)
+    with pytest.raises(ValueError):
+        lib.attn_rope(q, None, f, positions=_NoMemory(torch.full((9,), 7, dtype=torch.int32, device=DEV)))
+    c = lib.cache_empty(2, 2, 64, 64, DEV)
+    lengths = torch.tensor([9, 9], dtype=torch.int32, device=DEV)
+    counts = _NoMemory(torch.tensor([1, 2], dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        lib.attn_cache_append(c, q, q, lengths, counts)
+    with pytest.raises(ValueError):
+        lib.attn_cache_fwd(q, c, lengths, 0.125, counts=counts)
+    lse = torch.zeros(2, 2, 9, device=DEV)
+    with pytest.raises(ValueError):
+        lib.attn_cache_weights(q, c, lse, lengths, 0.125, weights=_NoMemory(torch.zeros(2, 2, 64, device=DEV)))
