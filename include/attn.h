@@ -338,6 +338,8 @@ int attn_fwd_ws(const void* Q, const void* K, const void* V, void* O, float* LSE
  *   frequencies      float64 [rot/2], device, radians per position (attn_rope_frequencies makes such a table)
  *   interleaved      0: pairs are columns (i, i + rot/2); otherwise (2i, 2i + 1)
  *   inverse          0: the rotation; otherwise the angles are negated, which (with the same magnitude) is its backward pass.
+ * ATTN_ERR_UNSUPPORTED where H + H_kv > 65535, B * N >= 2^31, or B * N > (2^24 - 1) * t, t the tokens of a work-group: 256 / s rounded down, with
+ * s = d / 4 (interleaved), (d - rot / 2) / 4 (rot a multiple of 8) or d - rot / 2.
  */
 int attn_rope(const void* Q, const void* K, void* Q_out, void* K_out, const long long* strides,
               const int* positions, long long positions_stride_b, const double* frequencies,

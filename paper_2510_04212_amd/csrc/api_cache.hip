@@ -13,7 +13,8 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-int launched(hipError_t e) { return e == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH; }
+// The dispatches return hipErrorInvalidConfiguration, before anything is launched, where a grid would be too large.
+int launched(hipError_t e) { return e == hipSuccess ? ATTN_OK : e == hipErrorInvalidConfiguration ? ATTN_ERR_UNSUPPORTED : ATTN_ERR_LAUNCH; }
 
 // Sizes of bf16 rows [B,H,N,d].  *empty for B * H == 0.
 int check_rows(int B, int H, int N, int d, bool* empty) {

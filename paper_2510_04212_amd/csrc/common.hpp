@@ -35,6 +35,9 @@ template <int N, class F> DEVI void static_for(F&& f) { static_for_impl(f, std::
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// HIP's limit: fewer than 2^32 threads along a dimension of the grid
+constexpr bool grid_fits(long long blocks, int threads) { return blocks < (1ll << 32) / threads; }
+
 DEVI f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }

@@ -115,6 +115,7 @@ template <int W, bool INTERLEAVED> hipError_t launch(RopeArgs p, hipStream_t str
   const int slots = INTERLEAVED ? p.d / W : p.rot / 2 / W + (p.d - p.rot) / W;
   const int per_block = kThreads / slots;
   const long long blocks = ((long long)p.B * p.N + per_block - 1) / per_block;
+  if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
   // Heads are shared out to several blocks until the grid fills the chip.  us, H 32/8, d 128, all heads in one block / as many blocks as 512 / 2048: 1 x 2048
   // tokens 23 / 10.5 / 9.9, 2 x 4096 - / 36 / 31, 1 x 512 19 / 4.4 / 5.0 (sines and cosines are formed again in each).
   const int heads = p.H + p.H_kv;

@@ -157,3 +157,15 @@ def test_rope_of_keys_alone_is_checked_like_any(binding):
     good, other = (1024, 512, 64), (4096, 2048, 64)
     assert rope(strides=_strides(*good, 1024, 512, 60, *good, *good)) == BAD and rope(strides=_strides(*good, *good, *good, 1024, 0, 64)) == BAD
     assert rope(Ko=_p(2), strides=_strides(*good, *good, *good, *other)) == BAD          # in place with other strides
+
+
+def test_rope_grids_beyond_the_limit(binding):
+    """Refused before they are launched: 2^32 threads along a dimension."""
+    lib = binding.raw()
+
+    def rope(N, d, rot, interleaved, B=1):
+        return lib.attn_rope(_p(1), None, _p(3), None, None, None, 0, _p(5), B, 1, 0, N, d, rot, interleaved, 1.0, 0, None)
+
+    assert rope(1 << 24, 256, 2, 0) == UNSUP and rope(1 << 12, 256, 2, 0, B=1 << 12) == UNSUP          # 255 threads a token
+    assert rope(1 << 24, 256, 250, 0) == UNSUP and rope(1 << 28, 96, 96, 1) == UNSUP                   # 131; 24: ten tokens a work-group
+    assert rope((1 << 30) - 63, 32, 32, 0) == UNSUP and rope(1 << 29, 32, 32, 1) == UNSUP              # 4: 64; 8: 32
