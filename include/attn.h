@@ -372,7 +372,7 @@ int attn_rope_frequencies(double* out, float* magnitude, int rot, double base, i
  *   K_scale, V_scale  float32 [B][H_kv][capacity/64]: a power of two for each block of 64 tokens of a head; V's is negative where the
  *                     block may hold NaN.
  * A code stands for its E4M3 value times the magnitude of its block's scale.  Memory need not be cleared: nothing behind a sequence's last
- * token is interpreted.  B * H_kv * capacity * d < 2^40, capacity <= 2^30.
+ * token is interpreted.  B * H_kv * capacity * d < 2^40, capacity <= 2^30, B and H_kv <= 65535.
  */
 #define ATTN_CACHE_BLOCK 64
 
@@ -383,6 +383,8 @@ int attn_rope_frequencies(double* out, float* magnitude, int rot, double base, i
  * the scale grows, older codes of the block are divided by what it grew by: exact but for codes that leave E4M3's normal range,
  * which are rounded again.  NaN stays NaN, an infinity (and a magnitude over 1.75 * 2^127) becomes the largest number of its block.
  *   strides  6 numbers on the HOST, or NULL: stride_b, stride_h, stride_n of K, V in elements; multiples of 8, >= 0
+ * ATTN_ERR_UNSUPPORTED where capacity = 2^30 and N > 2^30 - 127.
+ * Tokens at positions past the capacity are not stored: a cache that is full takes no more.
  * Blocks without a new token are left as they are; in those that begin with one, and where the scale grew, codes behind the last token become 0.
  */
 int attn_cache_append(const void* K, const void* V, const long long* strides, void* K_cache, void* V_cache,

@@ -1,6 +1,7 @@
 // Writing the 8-bit cache: new tokens quantised into it (attn_cache_append of include/attn.h), and a cache cut down to the
 // tokens that got the most attention (attn_cache_evict).
 #include "cache.hpp"
+#include <algorithm>
 
 namespace {
 
@@ -398,8 +399,10 @@ template <class F> hipError_t by_head_size(int d, F&& f) {
 }  // namespace
 
 hipError_t attn_cache_append_dispatch(const AppendArgs& p, int d, hipStream_t stream) {
-  // N tokens touch at most this many blocks, wherever they begin
-  const dim3 grid((unsigned)((p.N + kBlock - 2) / kBlock + 1), (unsigned)p.H_kv, (unsigned)p.B);
+  // N tokens touch at most this many blocks, wherever they begin; there are not more than the capacity's
+  const long long blocks = std::min(((long long)p.N + kBlock - 2) / kBlock + 1, (long long)(p.cache.capacity / kBlock));
+  if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks, (unsigned)p.H_kv, (unsigned)p.B);
   return by_head_size(d, [&](auto D) {
     attn_cache_append_kernel<D><<<grid, kThreads, 0, stream>>>(p);
     return hipGetLastError();

@@ -653,3 +653,14 @@ def test_weights_of_no_queries_are_refused(lib):
     q = torch.empty(2, 0, 5, 64, dtype=torch.bfloat16, device=DEV)
     with pytest.raises(ValueError):
         binding.attn_cache_weights(q, c, torch.empty(2, 0, 5, device=DEV), _i32([5, 9]), 0.125)
+
+
+def test_append_more_tokens_than_there_is_room_for(lib):
+    """2^31 - 1 new tokens (a view of one): those that would stand before the beginning do not exist."""
+    x = _bf16(_gen(61), 1, 1, 1, 32).to(DEV)
+    N = 2 ** 31 - 1
+    for cap, length in ((64, 64), (192, 130)):
+        many, few = _garbage(1, 1, cap, 32), _garbage(1, 1, cap, 32)
+        binding.attn_cache_append(many, x.expand(1, 1, N, 32), x.expand(1, 1, N, 32), _i32([length]))
+        binding.attn_cache_append(few, x.expand(1, 1, length, 32), x.expand(1, 1, length, 32), _i32([length]))
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(many, few))

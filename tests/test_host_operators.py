@@ -169,3 +169,9 @@ def test_rope_grids_beyond_the_limit(binding):
     assert rope(1 << 24, 256, 2, 0) == UNSUP and rope(1 << 12, 256, 2, 0, B=1 << 12) == UNSUP          # 255 threads a token
     assert rope(1 << 24, 256, 250, 0) == UNSUP and rope(1 << 28, 96, 96, 1) == UNSUP                   # 131; 24: ten tokens a work-group
     assert rope((1 << 30) - 63, 32, 32, 0) == UNSUP and rope(1 << 29, 32, 32, 1) == UNSUP              # 4: 64; 8: 32
+
+
+def test_append_grids_beyond_the_limit(binding):
+    lib = binding.raw()
+    for N in (1 << 30, (1 << 30) - 126, (1 << 31) - 1):
+        assert lib.attn_cache_append(_p(1), _p(2), None, _p(3), _p(4), _p(5), _p(6), _p(7), None, 1, 1, N, 32, 1 << 30, None) == UNSUP
