@@ -438,6 +438,7 @@ int attn_cache_weights(const void* Q, const long long* strides, const void* K_ca
  *                kept tokens, then 0
  *   kept         int32 [B][H_kv][budget]: the kept tokens' old positions, ascending, then -1
  *   K_out ...    the new cache; must not overlap the old one.  Blocks behind the last kept token are left as they are.
+ * ATTN_ERR_UNSUPPORTED where capacity_out = 2^30.
  * Afterwards the caller's lengths are min(lengths, budget).  Positions of later tokens for attn_rope go on counting from the old lengths.
  */
 int attn_cache_evict(const void* K_cache, const void* V_cache, const float* K_scale, const float* V_scale,

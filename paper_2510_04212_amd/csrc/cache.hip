@@ -410,6 +410,7 @@ hipError_t attn_cache_append_dispatch(const AppendArgs& p, int d, hipStream_t st
 }
 
 hipError_t attn_cache_evict_dispatch(const EvictArgs& p, int d, hipStream_t stream) {
+  if (!grid_fits(p.to.capacity / kBlock, kThreads)) return hipErrorInvalidConfiguration;         // (of the second kernel)
   // room for the longest sequence's keys if there is any, so that as many work-groups as possible share a compute unit (the whole call, 128 heads of 4400
   // weights: 84.0 us, and 86.4 with room for 32768; 512 of 8192: 391 and 395)
   const dim3 heads((unsigned)p.H_kv, (unsigned)p.B);

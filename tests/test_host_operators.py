@@ -175,3 +175,9 @@ def test_append_grids_beyond_the_limit(binding):
     lib = binding.raw()
     for N in (1 << 30, (1 << 30) - 126, (1 << 31) - 1):
         assert lib.attn_cache_append(_p(1), _p(2), None, _p(3), _p(4), _p(5), _p(6), _p(7), None, 1, 1, N, 32, 1 << 30, None) == UNSUP
+
+
+def test_evict_grids_beyond_the_limit(binding):
+    """Before the first of its kernels has written anything."""
+    lib = binding.raw()
+    assert lib.attn_cache_evict(*[_p(i + 1) for i in range(12)], 1, 1, 32, 1 << 20, 1 << 30, 100, 10, None) == UNSUP
