@@ -403,7 +403,7 @@ int attn_cache_append(const void* K, const void* V, const long long* strides, vo
  * A query that sees nothing, and queries i >= counts[b], give O = 0 and LSE = -infinity.  Scores, statistics and sums are float32, the row
  * sum that of the float32 probabilities; these are rounded to bf16 as the operand of the product with V, and O is rounded once.  A NaN among the values of a
  * token does not reach the queries that do not see it.  Deterministic; which float32 sums are formed in which order depends on the whole batch's lengths, as key blocks are shared out evenly over the chip.
- * ATTN_ERR_UNSUPPORTED, for attn_cache_weights as well, where B * H_kv * T * (capacity / 64 + 5) >= 2^30 (seconds of work), T the number of
+ * ATTN_ERR_UNSUPPORTED, for attn_cache_weights as well, where N * H >= 2^30, B * N * H >= 2^38, or B * H_kv * T * (capacity / 64 + 5) >= 2^30 (seconds of work), T the number of
  * tiles of 16, 64 or 128 that R = N H / H_kv rows make (R <= 16, <= 64, more).
  */
 size_t attn_cache_fwd_workspace_bytes(int B, int H, int H_kv, int N, int d, int capacity);
@@ -420,7 +420,7 @@ int attn_cache_fwd(const void* Q, const long long* strides, const void* K_cache,
  * float32 [B][H_kv][capacity]; weights of positions past the end become 0.  The call's own tokens (the last counts[b]) had
  * none: weights_in is not read for them.  weights_in NULL: nobody had any.  weights_out may be weights_in.  Q, strides (3 numbers, of Q),
  * lengths, counts, causal, softmax_scale as in the attn_cache_fwd call, LSE its output; rows whose LSE is -infinity add nothing.
- * Sums in float32, deterministic.
+ * Sums in float32, deterministic.  ATTN_ERR_UNSUPPORTED as for attn_cache_fwd, and where d = 256, capacity = 2^30 and R > 768.
  */
 int attn_cache_weights(const void* Q, const long long* strides, const void* K_cache, const float* K_scale,
                        const float* LSE, const int* lengths, const int* counts,

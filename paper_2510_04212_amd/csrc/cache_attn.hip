@@ -879,8 +879,10 @@ template <int D> hipError_t launch_weights(const WeighArgs& p, hipStream_t strea
     const long long blocks = (long long)p.B * p.H_kv * nb;
     const unsigned per_wave = (unsigned)std::min(8ll, std::max(1ll, blocks / 2048)), per_group = 4 * per_wave;
     attn_cache_weights_few_kernel<D><<<dim3((nb + per_group - 1) / per_group, (unsigned)p.H_kv, (unsigned)p.B), kThreads, 0, stream>>>(p, (int)per_wave);
-  } else
+  } else {
+    if (!grid_fits((nb + NB - 1) / NB, kThreads)) return hipErrorInvalidConfiguration;
     attn_cache_weights_many_kernel<D, NB><<<dim3((nb + NB - 1) / NB, (unsigned)p.H_kv, (unsigned)p.B), kThreads, 0, stream>>>(p);
+  }
   return hipGetLastError();
 }
 

@@ -181,3 +181,8 @@ def test_evict_grids_beyond_the_limit(binding):
     """Before the first of its kernels has written anything."""
     lib = binding.raw()
     assert lib.attn_cache_evict(*[_p(i + 1) for i in range(12)], 1, 1, 32, 1 << 20, 1 << 30, 100, 10, None) == UNSUP
+
+
+def test_weights_grids_beyond_the_limit(binding):
+    lib = binding.raw()
+    assert lib.attn_cache_weights(_p(1), None, _p(2), _p(3), _p(4), _p(5), None, _p(6), _p(7), 1, 1, 1, 769, 256, 1 << 30, 1, 0.125, None) == UNSUP
