@@ -484,8 +484,16 @@ def attn_bwd_rect(Q, K, V, O, dO, LSE, causal, softmax_scale, variant=STANDARD, 
 try:
     from . import _operators            # plain calls, marshalled in C++; None (False) from it: not a plain call, handled here
 except ImportError as e:
-    raise ImportError("the plain calls' marshalling is missing or does not fit this torch: build it with "
-                      "`python -m paper_2510_04212_amd.build`") from e
+    class _Missing:
+        """Attention needs nothing of it: the calls that do raise."""
+        def __init__(self, cause):
+            self.cause = cause
+
+        def __getattr__(self, name):
+            raise ImportError("the plain calls' marshalling is missing or does not fit this torch: build it with "
+                              "`python -m paper_2510_04212_amd.build`") from self.cause
+
+    _operators = _Missing(e)
 
 _PLAIN = (torch.Tensor, torch.nn.Parameter)
 CACHE_BLOCK = 64

@@ -186,3 +186,31 @@ def test_evict_grids_beyond_the_limit(binding):
 def test_weights_grids_beyond_the_limit(binding):
     lib = binding.raw()
     assert lib.attn_cache_weights(_p(1), None, _p(2), _p(3), _p(4), _p(5), None, _p(6), _p(7), 1, 1, 1, 769, 256, 1 << 30, 1, 0.125, None) == UNSUP
+
+
+def test_attention_does_without_the_marshalling_of_plain_calls():
+    """The binding imports where _operators does not (built for another torch, say); the calls that need it say so."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.modules['paper_2510_04212_amd._operators'] = None
+from paper_2510_04212_amd import binding
+assert binding.attn_fwd and binding.bwd_workspace_bytes(1, 2, 128, 64) > 0
+x = binding.torch.zeros((1, 1, 1, 64), dtype=binding.torch.bfloat16)
+c = binding.cache_empty(1, 1, 64, 64, device='cpu')
+f, _ = binding.rope_frequencies(64, device='cpu')
+for call in (lambda: binding.attn_rope(x, None, f), lambda: binding.attn_cache_append(c, x, x, None), lambda: binding.attn_cache_fwd(x, c, None, 1.0),
+             lambda: binding.attn_cache_weights(x, c, x, None, 1.0), lambda: binding.attn_cache_evict(c, x, x, 1, 0, out=c)):
+    try:
+        call()
+    except ImportError as e:
+        assert 'build' in str(e) and e.__cause__ is not None
+    else:
+        raise SystemExit('nothing raised')
+print('fine')
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "fine", r.stderr
