@@ -506,7 +506,8 @@ def rope_frequencies(rot, base=10000.0, scaling="none", factor=1.0, original_len
     the C ABI describes them."""
     if scaling not in _ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {', '.join(_ROPE_SCALINGS)}")
-    out = torch.empty(max(int(rot) // 2, 1), dtype=torch.float64)
+    _fit(int(rot))
+    out = torch.empty(min(max(int(rot) // 2, 1), 128), dtype=torch.float64)          # (rot above 256 is refused)
     magnitude = ctypes.c_float()
     _check(_lib.attn_rope_frequencies(_ptr(out), ctypes.byref(magnitude), int(rot), float(base), _ROPE_SCALINGS[scaling], float(factor),
                                       float(original_length), float(beta_fast), float(beta_slow)))

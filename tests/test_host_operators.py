@@ -214,3 +214,11 @@ print('fine')
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "fine", r.stderr
+
+
+def test_frequencies_of_sizes_beyond_int_are_refused(binding):
+    for rot in (2 ** 32 + 64, -2 ** 32 + 64):
+        with pytest.raises(ValueError):
+            binding.rope_frequencies(rot, device="cpu")
+    with pytest.raises(binding.AttnError):
+        binding.rope_frequencies(2 ** 31 - 2, device="cpu")
