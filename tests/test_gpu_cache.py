@@ -664,3 +664,89 @@ def test_append_more_tokens_than_there_is_room_for(lib):
         binding.attn_cache_append(many, x.expand(1, 1, N, 32), x.expand(1, 1, N, 32), _i32([length]))
         binding.attn_cache_append(few, x.expand(1, 1, length, 32), x.expand(1, 1, length, 32), _i32([length]))
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(many, few))
+
+
+# ---- forms that only longer caches, more segments and more rows reach
+
+def _filled_on_gpu(seed, B, Hkv, cap, d, lengths):
+    """As _filled, with keys whose blocks have scales of their own, too."""
+    g = torch.Generator(DEV).manual_seed(seed)
+
+    def rows(lo, hi):
+        gain = torch.exp2(torch.randint(lo, hi, (B, Hkv, cap // 64, 1, 1), generator=g, device=DEV).float())
+        x = torch.randn((B, Hkv, cap // 64, 64, d), generator=g, device=DEV)
+        return x.mul_(gain).to(torch.bfloat16).view(B, Hkv, cap, d)
+
+    c = _garbage(B, Hkv, cap, d)
+    binding.attn_cache_append(c, rows(-2, 1), rows(-3, 4), _i32(lengths), _i32(lengths))
+    return c
+
+
+def _check_rows(q, c, lengths, counts, alpha, O, lse, pairs, terms):
+    """Single queries of (sequence, key/value head) pairs against the oracle, causal.  terms: additions one after the other in a row's sum of
+    probabilities, 2^-24 each; 64 more for the joins (parts and waves) and the hardware exponential's 2^-22."""
+    H, N, d = q.shape[1:]
+    group = H // c.K.shape[1]
+    assert all((O[b, :, n:] == 0).all() and torch.isneginf(lse[b, :, n:]).all() for b, n in enumerate(counts))
+    for b, hk in pairs:
+        n, length = counts[b], lengths[b]
+        (K, V), (ek, ev) = _values(binding.Cache(*(t[b:b + 1, hk:hk + 1] for t in c)))
+        with np.errstate(invalid="ignore"):
+            K, V = ((x[0, 0] * np.repeat(2.0 ** e[0, 0], 64)[:, None])[:length] for x, e in ((K, ek), (V, ev)))
+        for i in sorted({*range(0, n, 13), n - 1} if n else ()):
+            seen = length - n + i + 1
+            for h in range(hk * group, (hk + 1) * group):
+                x = q[b, h, i:i + 1].double().cpu().numpy()
+                if seen <= 0:
+                    assert (O[b, h, i] == 0).all() and torch.isneginf(lse[b, h, i])
+                    continue
+                k, v = K[:seen], V[:seen]
+                o, l, size = oracle.attend(x, k, v, alpha, True)
+                e = (2 * (d + 4) * alpha * (np.abs(x) @ np.abs(k.T)).max() + terms + 64) * 2.0 ** -24 + 2.0 ** -22 * np.abs(alpha * x @ k.T).max()
+                assert abs(lse[b, h, i].item() - l[0]) <= e, (b, h, i)
+                off = np.abs(O[b, h, i].double().cpu().numpy() - o[0]) - (2.0 ** -8 * np.abs(o[0]) + (2.0 ** -8 + e) * 1.01 * (size[0] + np.abs(o[0])))
+                assert off.max() <= 0, (b, h, i, off.max(), off.argmax())
+
+
+@pytest.mark.parametrize("d", DIMS)
+@pytest.mark.parametrize("B,Hkv,group,N,cap", [
+    (17, 8, 2, 1, 4160),           # a wave's own blocks: segments in a few parts, as many shares as run at once
+    (41, 16, 1, 1, 4160),          # more segments than shares
+    (6, 8, 2, 20, 1280),           # blocks shared through LDS, one row tile a wave
+    (2, 8, 4, 300, 1280)])         # two, and ten tiles a sequence and head
+def test_parts_joined_by_two_waves(lib, d, B, Hkv, group, N, cap):
+    """Every segment is shared out (the call has a workspace), and in fewer than four parts on average."""
+    lengths = [cap if b % 5 == 0 else max(N, b * 977 % cap) for b in range(B)]
+    counts = [N if b % 2 == 0 else N - N // 3 for b in range(B)]
+    if B > 3:
+        lengths[3] = counts[3] = 0
+    c = _filled_on_gpu(d + N, B, Hkv, cap, d, lengths)
+    assert binding.cache_fwd_workspace_bytes(B, group * Hkv, Hkv, N, d, cap) > 0
+    q = _bf16(_gen(B), B, group * Hkv, N, d).to(DEV)
+    O, lse = binding.attn_cache_fwd(q, c, _i32(lengths), d ** -0.5, counts=_i32(counts))
+    # a lane adds 16 probabilities a block; a segment's blocks lie in one lane at most
+    _check_rows(q, c, lengths, counts, d ** -0.5, O, lse, [(b, h) for b in range(B) for h in (0, Hkv // 2 + 1)], cap // 4)
+
+
+@pytest.mark.parametrize("d", DIMS)
+@pytest.mark.parametrize("N", (20, 40))                    # 40 rows: one row tile a wave; 80: two
+def test_more_than_64_staged_blocks_of_a_segment(lib, d, N):
+    """72 full segments of 512 blocks on 512 work-groups (256 at d = 256): 72 blocks or more each, whose scales come 64 at a time."""
+    B, Hkv, group, cap = 9, 8, 2, 32768
+    c = _filled_on_gpu(d + N, B, Hkv, cap, d, [cap] * B)
+    q = _bf16(_gen(N), B, group * Hkv, N, d).to(DEV)
+    O, lse = binding.attn_cache_fwd(q, c, _i32([cap] * B), d ** -0.5)
+    _check_rows(q, c, [cap] * B, [N] * B, d ** -0.5, O, lse, [(0, 0), (0, 1), (4, 3), (8, 7)], 16 * 512)
+
+
+def test_evict_more_weights_than_fit_into_lds(lib):
+    """32768 weights in front of the recent ones stay in LDS, one more does not; ends inside a thread's four."""
+    g = _gen(41)
+    lengths, cap = [32868, 32869, 39999], 40000
+    c = _filled(g, 3, 1, cap, 32, lengths)
+    spread = torch.exp(2 * torch.randn((3, 1, cap), generator=g))
+    tied = torch.randint(0, 4, (3, 1, cap), generator=g).float() * 0.25
+    tied[1, 0, ::3] = -0.0
+    for w in (spread, tied):
+        for budget, recent in ((5000, 100), (33000, 0), (1, 0)):
+            _check_evict(c, w.to(DEV), lengths, budget, recent)
