@@ -354,7 +354,8 @@ int attn_rope(const void* Q, const void* K, void* Q_out, void* K_out, const long
  *   ATTN_ROPE_NTK     base * factor^(rot/(rot-2)) in place of base (rot >= 4): the lowest frequency is divided by factor, the highest kept
  *   ATTN_ROPE_YARN    by parts: with r = original_length * frequency / (2 pi) turns over the trained length, frequencies of
  *                     r >= beta_fast are kept, those of r <= beta_slow divided by factor, those between mixed linearly in r
- *                     ("YaRN: Efficient Context Window Extension of Large Language Models"); *magnitude = 0.1 ln(factor) + 1,
+ *                     ("YaRN: Efficient Context Window Extension of Large Language Models"; a checkpoint trained with
+ *                     another ramp, linear in i for instance, needs a table of its own); *magnitude = 0.1 ln(factor) + 1,
  *                     the factor on queries and keys that goes with it.  beta_fast > beta_slow >= 0 (the paper: 32 and 1).
  * *magnitude (may be NULL) is 1 for the others.
  */

@@ -24,7 +24,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 // d = 32 c + 8 half + ... of the columns: 16-byte chunks serve 64 columns (lane group g: 16 g ..), an 8-byte one the last 32 (8 g ..)
 template <int D> struct Cols {
-  static constexpr int C64 = D / 64, KC = D / 32;          // whole chunks, and instructions of K Q^T
+  static constexpr int C64 = D / 64;       // whole chunks
   static constexpr bool ODD = D % 64 != 0;
 };
 

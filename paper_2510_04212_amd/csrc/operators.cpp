@@ -32,7 +32,7 @@ bool on(const Tensor& t, Device device, at::ScalarType type) {
   return t.defined() && t.is_cuda() && t.layout() == at::kStrided && t.scalar_type() == type && t.get_device() == device && !t.is_neg() &&
          !t.is_conj() && t.data_ptr() != nullptr;
 }
-// bf16 rows [B,H,N,d] the library takes as they are; least: of a stride
+// bf16 rows [B,H,N,d] the library takes as they are
 bool rows(const Tensor& t, Device device) {
   if (!on(t, device, at::kBFloat16) || t.dim() != 4 || t.numel() == 0 || t.stride(3) != 1) return false;
   if (reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 != 0) return false;
