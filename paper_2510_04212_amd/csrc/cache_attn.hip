@@ -9,7 +9,8 @@
 //   so that S^T leaves lane group g with the 16 consecutive tokens 16 g .. 16 g + 15 of the block, which are the k-slots that V's
 //   16 bytes of column 16 dt + r have: 8 of them make one instruction's, the other 8 the next one's.
 // The row sum adds the float32 probabilities, not the rounded ones that are multiplied with V: LSE is exact to float32, as the weights
-// exp(S - LSE) need it.
+// exp(S - LSE) need it.  P is rounded to bf16 for that product because the matrix unit takes 16-bit operands: O's relative error (root mean square, against
+// 64 bits) is 0.0022, and 0.0017, O's own rounding, with P in float32, which would take a second product of every tile.
 //
 // Rows.  All query heads of a key/value head share its cache: their queries are one list of rows, row = query * group + head of the
 // group, cut into tiles of M = 16 RT 4 / KW rows.  A work-group's four waves take KW shares of the key blocks of 4 / KW row groups.
@@ -268,8 +269,8 @@ DEVI void take_out_nan(Acc<D, RT>& a, VCodes<D>& v, const int (&limit)[RT], int 
 // bf16 alike), so that the accumulators are hardly ever rescaled.
 //
 // Of the two waves that share a SIMD, the one that multiplies goes first, so that the other's softmax fills in (2048 queries over 16384 tokens, H 32/8,
-// d 128: 632 -> 600 us; 16 queries of 64 sequences of 4300: 128 -> 120; d = 64, 4096 queries of 4 sequences: 463 -> 422; with one wave a SIMD, d = 256: 243 ->
-// 248, not there).
+// d 128: 534 -> 493 us; 16 queries of 64 sequences of 4300: 126 -> 121; d = 64, 4096 queries of 4 sequences: 441 -> 413; with one wave a SIMD, d = 256, even:
+// not there).
 constexpr float kSlack = 8.f;
 template <int D, int RT, class F>
 DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, float scale_log2,
@@ -350,9 +351,10 @@ DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
 //
 // KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead (one token of 64 sequences of 4300, H 32/8, d
-// 128: 103 us, 5.5 TB/s).  KW = 1, many rows: bound by
+// 128: 100 us, 5.6 TB/s).  KW = 1, many rows: bound by
 // the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers a block ahead (three blocks ahead, in four
-// buffers: 16 queries of 64 sequences of 4300 tokens, H 32/8, d 128, 139 us; one ahead, in two: 125.  2048 queries over 16384: 636 and 620).
+// buffers: 16 queries of 64 sequences of 4300 tokens, H 32/8, d 128, 139 us; one ahead, in two: 125.  2048 queries over 16384: 636 and 620; these with the
+// loop of that time, which takes 121 and 493 now).
 template <int D, int RT, int KW, bool SPLIT>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
   constexpr int RG = 4 / KW, M = 16 * RT * RG;
@@ -663,7 +665,7 @@ template <int D> hipError_t launch_fwd(const AttendArgs& p, hipStream_t stream) 
 //
 // Few row tiles: bound by K's bytes; a wave takes up to 8 blocks one after the other, the next one's codes on their way (one token of 32
 // sequences of 2000 to 4160 tokens, H 32/8, d 128: 25 us with a block per wave, 22.6 with 2, 21.4 with 8).  Many: by the exponentials and the products, and by what a row
-// tile costs besides (addresses, loads), which two blocks share (500 queries, H 32/8, over 16384 tokens: 156 us with one block, 95 with two);
+// tile costs besides (addresses, loads), which two blocks share (500 queries, H 32/8, over 16384 tokens: 142 us with one block, 80 with two);
 // the four waves of a work-group take the row tiles in turn.
 DEVI float sum_over_16_lanes(float x) {        // the same in all 16: four rotations of the row
   x += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, false));
@@ -872,8 +874,9 @@ template <int D> hipError_t launch_weights(const WeighArgs& p, hipStream_t strea
   const unsigned nb = (unsigned)(p.cache.capacity / kBlock);
   constexpr int NB = D <= 128 ? 2 : 1;       // (a lane's registers hold one block's keys of d = 256)
   // The crossing point is where the second block's widened keys are paid for, later the more there are of them.  us, few / many, 32 sequences of 4096
-  // (d = 128; 16 of d = 32, 64; 8 of d = 256): 96 rows 76 / 119, 256 151 / 167, 384 210 / 204, 512 264 / 250, 1024 516 / 375; d = 32: 96 rows 19.2 / 20.8, 128
-  // 23.4 / 22.4; d = 64: 128 27 / 30, 192 37.4 / 36.7, 256 47 / 42; d = 256: 96 38 / 59, 512 132 / 151.
+  // (d = 96, 128; 16 of d = 32, 64; 8 of d = 256): d = 128: 256 rows 141 / 159, 320 171 / 177, 384 202 / 199, 448 232 / 226, 512 264 / 246; d = 32: 96 rows
+  // 18.3 / 19.5, 128 22.8 / 21.7; d = 64: 160 32.6 / 33.7, 192 37.6 / 36.5, 256 47 / 43; d = 96: 288 123 / 126, 320 135 / 133.  At d = 256 it lies beyond
+  // the rule's 768: 512 133 / 151, 768 194 / 208, 896 225 / 237.
   if ((long long)p.N * p.group <= 3 * D) {
     // a block per wave until the waves are two to a SIMD, then more, up to 8
     const long long blocks = (long long)p.B * p.H_kv * nb;

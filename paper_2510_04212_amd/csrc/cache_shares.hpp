@@ -142,6 +142,7 @@ template <int KW> constexpr int kLeastUnits = kStart + (KW == 4 ? 1 : 2);
 inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
   return (double)B * H_kv * f.tiles * (kStart + capacity / kBlock);
 }
+// Figures come in pairs, both sides measured on the code of that step; later steps made both faster.
 // Rows.  Up to 16: each wave takes blocks of its own (one token of 64 sequences of 4300, H 32/8, d 128: 102 us, and 116 with the blocks
 // shared through LDS; of 4 sequences of 1000: 13 and 24).  From 17 on the blocks would be read and widened once for each row tile: the waves share
 // them (32 rows of 64 x 4300: 132 us with blocks of a wave's own, 118 shared; 64 rows: 164 and 123).  From 65 on two row tiles a wave (68 rows:

@@ -2,7 +2,7 @@
 //
 // What bounds a token's step is the host: rotating, appending or attending for one token takes the GPU 4 to 7 us, and the checks, ctypes
 // conversions and allocations of binding.py took longer.  us a call among others, in Python -> here: rotating one token of 32 sequences
-// 17.4 -> 5.6, appending it 12.4 -> 6.6, attending to 1024 tokens of one sequence 16.4 -> 5.8.
+// 17.4 -> 5.7, appending it 12.4 -> 6.1, attending to 1024 tokens of one sequence 16.4 -> 5.8.
 //
 // Each function takes the plain case - tensors on the current GPU, of the types, shapes, strides and alignments that binding.py and the library
 // accept, outputs and workspace new, on the current stream - and returns None for any other: the caller's Python code then handles it, or raises
