@@ -447,6 +447,82 @@ int attn_cache_evict(const void* K_cache, const void* V_cache, const float* K_sc
                      void* K_out, void* V_out, float* K_scale_out, float* V_scale_out, float* weights_out, int* kept,
                      int B, int H_kv, int d, int capacity, int capacity_out, int budget, int recent, void* stream);
 
+/*
+ * ---- One prompt, many continuations: answers sampled side by side, beams, conversations that begin with the same instructions.
+ *
+ * What the sequences have in common is a prefix, in a cache of P sequences; each of S sequences of a prefix has a cache for what follows: sequence
+ * b of the P * S (<= 65535) continues prefix b / S.  Attention reads a prefix once for all of them; sequences are copied to another cache or to
+ * other places of their own; and the best of all beams' next tokens are chosen.
+ */
+
+/*
+ * attn_cache_fwd for such sequences: query i of sequence b sees, if i < counts[b], all min(prefix_lengths[b / S], prefix_capacity) tokens of its prefix
+ * (none where that is negative) and, of its own cache, the tokens that attn_cache_fwd says; O and LSE are those of one softmax over both.  Rotary
+ * positions of a sequence's own tokens begin at the prefix's length, which is the caller's matter.
+ *   Q, O     bf16 [P * S,H,N,d];  LSE float32 [P * S,H,N];  strides, lengths, counts, causal, workspace: as in attn_cache_fwd
+ *   K_prefix, V_prefix, K_prefix_scale, V_prefix_scale   a cache of P sequences, of prefix_capacity tokens each
+ *   prefix_lengths  int32 [P], device
+ * Everything else is as in attn_cache_fwd: rounding, statistics and sums, what sees nothing, NaN among values, determinism.
+ * ATTN_ERR_UNSUPPORTED also where P * S > 65535, N * H * S >= 2^30, P * S * H_kv * T * ((prefix_capacity + capacity) / 64 + 5) >= 2^30 or T > 65535, with T of
+ * attn_cache_fwd.
+ */
+size_t attn_cache_fwd_shared_workspace_bytes(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity);
+int attn_cache_fwd_shared(const void* Q, const long long* strides, const void* K_prefix, const void* V_prefix,
+                          const float* K_prefix_scale, const float* V_prefix_scale, const int* prefix_lengths,
+                          const void* K_cache, const void* V_cache, const float* K_scale, const float* V_scale,
+                          const int* lengths, const int* counts, void* O, float* LSE, void* workspace,
+                          size_t workspace_bytes, int P, int S, int H, int H_kv, int N, int d, int prefix_capacity,
+                          int capacity, int causal, float softmax_scale, void* stream);
+
+/*
+ * A cache of B_out sequences that are copies of sequences of another, of B: sequence i holds the first
+ *   lengths_out[i] = min(lengths[s], capacity, capacity_out)
+ * tokens of s = sources[i] (0 where that or s is negative, or s >= B).  The same source may be named any number of times, or never: forks of
+ * a prompt, a batch without the sequences that have ended, a cache of another capacity.  Whole blocks are copied, codes and scales as
+ * they are; blocks behind the last copied token are left as they are.
+ *   sources      int32 [B_out], lengths int32 [B], lengths_out int32 [B_out], device
+ *   K_out ...    must not overlap the cache that is copied
+ */
+int attn_cache_fork(const void* K_cache, const void* V_cache, const float* K_scale, const float* V_scale,
+                    const int* sources, const int* lengths, void* K_out, void* V_out, float* K_scale_out,
+                    float* V_scale_out, int* lengths_out, int B, int B_out, int H_kv, int d, int capacity,
+                    int capacity_out, void* stream);
+
+/*
+ * Sequences of a cache replaced, in place, by others of their group: sequence g * S + s of P * S (<= 65535) becomes what sequence
+ * g * S + parents[g * S + s] was before the call, and lengths_out[g * S + s] its length, whatever permutation or copies parents describe.  A sequence
+ * that is its own parent costs nothing; where parents is outside 0 .. S - 1 the sequence stays as it is.  Blocks behind the last token of
+ * what is copied are left as they are.  S <= 64.
+ *   parents, lengths  int32 [P * S], device;  lengths_out int32 [P * S], another array
+ */
+int attn_cache_reorder(void* K_cache, void* V_cache, float* K_scale, float* V_scale, const int* parents,
+                       const int* lengths, int* lengths_out, int P, int S, int H_kv, int d, int capacity,
+                       void* stream);
+
+/*
+ * The choice among beams.  Token t continues beam k of item b with the sum  scores[b][k] + x_t - log(sum_u exp(x_u)),  x the beam's logits; the n
+ * (<= 128) largest sums of an item's beams * V are its next beams, the largest first: parents (the beam they continue), tokens, and the sums, float32 [B][n].
+ * Equal sums: the lower beam first, and within a beam the larger logit, then the lower token.  Sums are formed and compared in float64, from a
+ * float32 sum of exponentials (float64 over more than 32 of them).
+ *   logits       ATTN_LOGITS_BF16 or ATTN_LOGITS_FLOAT32; token t of beam k of item b at element b * stride_b + k * stride_beam + t (>= 0), aligned as its type
+ *   finished     1 byte [B][beams] or NULL: a beam with a value other than 0 has ended.  Its logits are not read; it has one continuation,
+ *                end_token, which adds nothing to its score.
+ *   end_token    the token that ends a sequence; negative: none (finished must be NULL then)
+ *   finished_out 1 byte [B][n] or NULL: 1 where the token is end_token or the beam had ended, otherwise 0
+ * A logit of -infinity is no continuation.  A beam with a logit that is NaN or +infinity, without one above -infinity, or with a score that is not finite
+ * has none.  Places without a continuation: parent and token -1, sum -infinity, finished_out 0.
+ *   workspace    attn_beam_select_workspace_bytes(...) bytes, 16-byte aligned; contents on entry are ignored; free for reuse once the stream has passed the
+ *                call.  Calls that can overlap in time need one each.
+ * beams <= 64, V <= 2^24, B <= 2^20, and ATTN_ERR_UNSUPPORTED where B * beams * V makes a grid beyond the runtime's limit (some 10^10 logits).
+ */
+#define ATTN_LOGITS_BF16 0
+#define ATTN_LOGITS_FLOAT32 1
+size_t attn_beam_select_workspace_bytes(int B, int beams, int V, int n);
+int attn_beam_select(const void* logits, int logits_type, long long stride_b, long long stride_beam,
+                     const float* scores, const unsigned char* finished, int end_token, int* parents, int* tokens,
+                     float* scores_out, unsigned char* finished_out, void* workspace, size_t workspace_bytes, int B,
+                     int beams, int V, int n, void* stream);
+
 /* Human-readable name of an attn_status (static storage, never NULL). */
 const char* attn_status_string(int status);
 

@@ -85,6 +85,18 @@ _lib.attn_cache_weights.argtypes = [_vp] * 9 + [_i] * 7 + [_f, _vp]
 _lib.attn_cache_weights.restype = _i
 _lib.attn_cache_evict.argtypes = [_vp] * 12 + [_i] * 7 + [_vp]
 _lib.attn_cache_evict.restype = _i
+_lib.attn_cache_fwd_shared.argtypes = [_vp] * 16 + [_sz] + [_i] * 9 + [_f, _vp]
+_lib.attn_cache_fwd_shared.restype = _i
+_lib.attn_cache_fwd_shared_workspace_bytes.argtypes = [_i] * 8
+_lib.attn_cache_fwd_shared_workspace_bytes.restype = _sz
+_lib.attn_cache_fork.argtypes = [_vp] * 11 + [_i] * 6 + [_vp]
+_lib.attn_cache_fork.restype = _i
+_lib.attn_cache_reorder.argtypes = [_vp] * 7 + [_i] * 5 + [_vp]
+_lib.attn_cache_reorder.restype = _i
+_lib.attn_beam_select.argtypes = [_vp, _i, _ll, _ll, _vp, _vp, _i] + [_vp] * 5 + [_sz] + [_i] * 4 + [_vp]
+_lib.attn_beam_select.restype = _i
+_lib.attn_beam_select_workspace_bytes.argtypes = [_i] * 4
+_lib.attn_beam_select_workspace_bytes.restype = _sz
 _lib.attn_status_string.argtypes = [_i]
 _lib.attn_status_string.restype = ctypes.c_char_p
 _lib.attn_fwd_key_tile.argtypes = [_i]
@@ -100,7 +112,9 @@ EXPORTS = ["attn_fwd", "attn_fwd_ex", "attn_fwd_opt", "attn_delta", "attn_delta_
            "attn_fwd_gqa", "attn_bwd_gqa", "attn_fwd_rect", "attn_bwd_rect",
            "attn_bwd_workspace_bytes", "attn_fwd_ws", "attn_fwd_workspace_bytes",
            "attn_status_string", "attn_fwd_key_tile", "attn_rope", "attn_rope_frequencies", "attn_cache_append",
-           "attn_cache_fwd", "attn_cache_fwd_workspace_bytes", "attn_cache_weights", "attn_cache_evict"]
+           "attn_cache_fwd", "attn_cache_fwd_workspace_bytes", "attn_cache_weights", "attn_cache_evict",
+           "attn_cache_fwd_shared", "attn_cache_fwd_shared_workspace_bytes", "attn_cache_fork", "attn_cache_reorder",
+           "attn_beam_select", "attn_beam_select_workspace_bytes"]
 
 
 class AttnError(RuntimeError):
@@ -770,3 +784,129 @@ def attn_cache_evict(cache, weights, lengths, budget, recent, out=None, stream=N
                                  _ptr(out.K), _ptr(out.V), _ptr(out.K_scale), _ptr(out.V_scale), _ptr(weights_out), _ptr(kept), B, H_kv, d,
                                  capacity, capacity_out, int(budget), int(recent), _stream(stream)))
     return out, weights_out, kept
+
+
+# ---- one prompt, many continuations
+
+def _workspace(workspace, need, device, stream):
+    """(workspace, its bytes): the caller's, or a new one where the call needs any."""
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.device != device:
+            raise ValueError(f"workspace must be a contiguous tensor on {device}")
+        return workspace, workspace.numel() * workspace.element_size()
+    if need > 0:
+        workspace = _on(device, stream, lambda: torch.empty(need, dtype=torch.uint8, device=device))
+    return workspace, need
+
+
+def cache_fwd_shared_workspace_bytes(P, S, H, H_kv, N, d, prefix_capacity, capacity):
+    """Workspace that attn_cache_fwd_shared needs for this problem (0: none)."""
+    _fit(P, S, H, H_kv, N, d, prefix_capacity, capacity)
+    return int(_lib.attn_cache_fwd_shared_workspace_bytes(P, S, H, H_kv, N, d, prefix_capacity, capacity))
+
+
+def attn_cache_fwd_shared(Q, prefix, prefix_lengths, cache, lengths, softmax_scale, causal=True, counts=None, O=None, LSE=None, workspace=None,
+                          stream=None):
+    """O, LSE = attn_cache_fwd for sequences that continue shared prefixes: `prefix` is a Cache of P sequences, `cache` one of P * S, and sequence b
+    continues prefix b // S.  Query i < counts[b] sees all prefix_lengths[b // S] tokens (int32 [P]) of its prefix, and of its own
+    what attn_cache_fwd says; a prefix is read once for all its sequences.
+
+    Everything else is as in attn_cache_fwd; the workspace has cache_fwd_shared_workspace_bytes(...) bytes."""
+    B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
+    P, Hp, prefix_capacity, dp, device_p = _cache_shape(prefix, "prefix")
+    if (Hp, dp, device_p) != (H_kv, d, device) or (P == 0) != (B == 0) or (P and B % P):
+        raise ValueError("prefix must have the heads and head size of the cache, and one sequence for every so many of its sequences")
+    S = B // P if P else 0
+    _dense(prefix_lengths, "prefix_lengths", (P,), torch.int32, device)
+    _sequence_lengths(lengths, counts, B, device)
+    if O is None:
+        O = _on(device, stream, lambda: torch.empty((B, H, N, d), dtype=Q.dtype, device=device))
+    elif _rows(O, "O") != Q.shape:
+        raise ValueError("O must have the shape of Q")
+    if LSE is None:
+        LSE = _on(device, stream, lambda: torch.empty((B, H, N), dtype=torch.float32, device=device))
+    else:
+        _dense(LSE, "LSE", (B, H, N), torch.float32, device)
+    workspace, size = _workspace(workspace, cache_fwd_shared_workspace_bytes(P, S, H, H_kv, N, d, prefix_capacity, capacity), device, stream)
+    _check(_lib.attn_cache_fwd_shared(_ptr(Q), _strides(Q, O), _ptr(prefix.K), _ptr(prefix.V), _ptr(prefix.K_scale), _ptr(prefix.V_scale),
+                                      _ptr(prefix_lengths), _ptr(cache.K), _ptr(cache.V), _ptr(cache.K_scale), _ptr(cache.V_scale), _ptr(lengths),
+                                      _ptr_or_none(counts), _ptr(O), _ptr(LSE), _ptr_or_none(workspace), size, P, S, H, H_kv, N, d, prefix_capacity,
+                                      capacity, int(bool(causal)), float(softmax_scale), _stream(stream)))
+    return O, LSE
+
+
+def attn_cache_fork(cache, sources, lengths, out=None, stream=None):
+    """(out, lengths_out): a cache whose sequence i is a copy of sequence sources[i] (int32 [B_out]) of `cache`, which has lengths[sources[i]] tokens
+    (int32 [B]), cut off at the capacity of `out`; empty where sources[i] is outside the cache.  Forks of a prompt, a batch without
+    the sequences that have ended, a cache of another capacity.
+
+    out: another Cache of len(sources) sequences; a new one of the same capacity when absent."""
+    B, H_kv, capacity, d, device = _cache_shape(cache)
+    _dense(lengths, "lengths", (B,), torch.int32, device)
+    if sources.dim() != 1:
+        raise ValueError("sources must be an int32 tensor [B_out]")
+    _dense(sources, "sources", sources.shape, torch.int32, device)
+    if out is None:
+        out = _on(device, stream, lambda: cache_empty(sources.shape[0], H_kv, capacity, d, device))
+    B_out, Ho, capacity_out, do, device_out = _cache_shape(out, "out")
+    if (B_out, Ho, do, device_out) != (sources.shape[0], H_kv, d, device):
+        raise ValueError("out must have a sequence for each of sources, and the heads and head size of the cache")
+    lengths_out = _on(device, stream, lambda: torch.empty((B_out,), dtype=torch.int32, device=device))
+    _check(_lib.attn_cache_fork(_ptr(cache.K), _ptr(cache.V), _ptr(cache.K_scale), _ptr(cache.V_scale), _ptr(sources), _ptr(lengths), _ptr(out.K),
+                                _ptr(out.V), _ptr(out.K_scale), _ptr(out.V_scale), _ptr(lengths_out), B, B_out, H_kv, d, capacity, capacity_out,
+                                _stream(stream)))
+    return out, lengths_out
+
+
+def attn_cache_reorder(cache, parents, lengths, stream=None):
+    """lengths_out: int32 [P * S], after the sequences of `cache` have been replaced, in place, by others of their group of S: sequence g * S + s by
+    what g * S + parents[g, s] was (int32 [P,S], S <= 64), as attn_beam_select's parents say it.  Values outside 0 .. S - 1 leave a sequence
+    as it is; lengths: int32 [P * S]."""
+    B, H_kv, capacity, d, device = _cache_shape(cache)
+    if parents.dim() != 2 or parents.numel() != B:
+        raise ValueError("parents must be an int32 tensor [P,S] with a value for each sequence of the cache")
+    P, S = parents.shape
+    _dense(parents, "parents", (P, S), torch.int32, device)
+    _dense(lengths, "lengths", (B,), torch.int32, device)
+    lengths_out = _on(device, stream, lambda: torch.empty((B,), dtype=torch.int32, device=device))
+    _check(_lib.attn_cache_reorder(_ptr(cache.K), _ptr(cache.V), _ptr(cache.K_scale), _ptr(cache.V_scale), _ptr(parents), _ptr(lengths),
+                                   _ptr(lengths_out), P, S, H_kv, d, capacity, _stream(stream)))
+    return lengths_out
+
+
+def beam_select_workspace_bytes(B, beams, V, n):
+    """Workspace that attn_beam_select needs for this problem."""
+    _fit(B, beams, V, n)
+    return int(_lib.attn_beam_select_workspace_bytes(B, beams, V, n))
+
+
+def attn_beam_select(logits, scores, n, finished=None, end_token=None, workspace=None, stream=None):
+    """(parents, tokens, sums, ended), [B,n] each: the n (<= 128) continuations with the largest scores[b,k] + log_softmax(logits[b,k])[t] of each
+    item's beams, the largest first (equal ones: the lower beam, then the lower token), as int32, int32, float32 and bool.
+
+    logits: float32 or bfloat16 [B,beams,V] with a contiguous last dimension; scores: float32 [B,beams].  finished: bool [B,beams], beams that
+    have ended: they continue with end_token alone, which adds nothing to their score.  ended: whether a continuation is, or had come to, an end.
+    Logits of -infinity are never chosen; a beam with a NaN or +infinity, or whose score is not finite, has no continuation.  Where there are fewer
+    than n, the rest of parents and tokens is -1, and of the sums -infinity."""
+    if logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda or logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] > 1):
+        raise ValueError("logits must be a CUDA float32 or bfloat16 tensor [B,beams,V] whose last dimension is contiguous")
+    device = logits.device
+    if logits.get_device() != torch.cuda.current_device():
+        raise ValueError("logits must be on the current GPU")
+    B, beams, V = logits.shape
+    _fit(B, beams, V, n, -1 if end_token is None else end_token)
+    if n < 0 or (end_token is not None and not 0 <= end_token < max(V, 1)):
+        raise ValueError("n must not be negative, and end_token be a token")
+    _dense(scores, "scores", (B, beams), torch.float32, device)
+    if finished is not None:
+        _dense(finished, "finished", (B, beams), torch.bool, device)
+        if end_token is None:
+            raise ValueError("finished beams need an end_token")
+    new = lambda dtype: _on(device, stream, lambda: torch.empty((B, n), dtype=dtype, device=device))
+    parents, tokens, sums, ended = new(torch.int32), new(torch.int32), new(torch.float32), new(torch.bool)
+    workspace, size = _workspace(workspace, beam_select_workspace_bytes(B, beams, V, n), device, stream)
+    stride = lambda i: logits.stride(i) if logits.shape[i] > 1 else 0
+    _check(_lib.attn_beam_select(_ptr(logits), int(logits.dtype == torch.float32), stride(0), stride(1), _ptr(scores), _ptr_or_none(finished),
+                                 -1 if end_token is None else end_token, _ptr(parents), _ptr(tokens), _ptr(sums), _ptr(ended), _ptr_or_none(workspace),
+                                 size, B, beams, V, n, _stream(stream)))
+    return parents, tokens, sums, ended

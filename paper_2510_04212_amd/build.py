@@ -4,7 +4,7 @@ One hipcc invocation per source (gfx950 only).  Four libraries come out:
   libattn_gfx950.so         the attention library (the C ABI of include/attn.h);
   libattn_probe_gfx950.so   measurement aids that only the benchmark loads (csrc/probe.h);
   _autograd.so              the autograd node of attention() (host code, linked against the first);
-  _operators.so             plain calls of the rotary positions and the 8-bit cache (the same).
+  _operators.so             plain calls of the rotary positions, the 8-bit cache and the choice among beams (the same).
 Packed-fp32 code generation is switched off for all device code.
 """
 import os
@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libattn_gfx950.so")
 PROBE_LIB = os.path.join(HERE, "libattn_probe_gfx950.so")
 NODES = ["autograd", "operators"]              # csrc/NAME.cpp -> _NAME.so
-SOURCES = ["api.hip", "fwd.hip", "delta.hip", "bwd.hip", "api_cache.hip", "rope.hip", "cache.hip", "cache_attn.hip"]
+SOURCES = ["api.hip", "fwd.hip", "delta.hip", "bwd.hip", "api_cache.hip", "rope.hip", "cache.hip", "cache_attn.hip", "cache_shared.hip",
+           "cache_copy.hip", "beam.hip"]
 PROBE_SOURCES = ["probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -37,7 +38,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # The backward loses by it (dK/dV B2 H8 N2048 122 -> 131, dQ even).  Attention over the 8-bit cache gains by it at the same head size (2048 queries of 4
 # sequences 300 -> 256), others as before.
 EXTRA_FLAGS = {"bwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"], "fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-               "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+               "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "cache_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _node_command(name):

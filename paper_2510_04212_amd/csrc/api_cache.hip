@@ -1,9 +1,10 @@
-// C ABI of the rotary positions and of the 8-bit cache (see include/attn.h): argument validation and dispatch only.
+// C ABI of the rotary positions, of the 8-bit cache and of the choice among beams (see include/attn.h): argument validation and dispatch only.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <algorithm>
 #include <cmath>
 #include "../../include/attn.h"
+#include "beam.hpp"
 #include "cache.hpp"
 #include "rope.hpp"
 
@@ -265,4 +266,180 @@ extern "C" int attn_cache_evict(const void* K_cache, const void* V_cache, const 
   a.lengths = lengths;
   a.B = B; a.H_kv = H_kv; a.budget = budget; a.recent = recent;
   return launched(attn_cache_evict_dispatch(a, d, static_cast<hipStream_t>(stream)));
+}
+
+// The work that a call of P * S sequences can be, in key blocks of row tiles, in whichever form.
+static int check_shared(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity, bool* empty) {
+  *empty = false;
+  if (P < 0 || S < 0) return ATTN_ERR_BAD_ARG;
+  if (P > 65535 || S > 65535 || (double)P * S > 65535.0) return ATTN_ERR_UNSUPPORTED;
+  int st = check_attend(P * S, H, H_kv, N, d, capacity, empty);
+  if (st != ATTN_OK || *empty) return st;
+  if ((st = check_cache(P, H_kv, d, prefix_capacity)) != ATTN_OK) return st;
+  if ((double)N * H * S >= 1073741824.0) return ATTN_ERR_UNSUPPORTED;      // rows of a prefix: counted in int
+  const CacheForm f = cache_form(P * S, H, H_kv, N, d, capacity);
+  const double units = cache_units(P * S, H_kv, f, capacity) + (double)P * S * H_kv * f.tiles * (prefix_capacity / kBlock);
+  return f.tiles <= 65535 && units < kUnitLimit ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
+}
+
+extern "C" size_t attn_cache_fwd_shared_workspace_bytes(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity) {
+  bool empty;
+  if (check_shared(P, S, H, H_kv, N, d, prefix_capacity, capacity, &empty) != ATTN_OK || empty) return 0;
+  return attn_cache_fwd_shared_partial_bytes(P, S, H, H_kv, N, d, prefix_capacity, capacity);
+}
+
+extern "C" int attn_cache_fwd_shared(const void* Q, const long long* strides, const void* K_prefix, const void* V_prefix, const float* K_prefix_scale,
+                                     const float* V_prefix_scale, const int* prefix_lengths, const void* K_cache, const void* V_cache,
+                                     const float* K_scale, const float* V_scale, const int* lengths, const int* counts, void* O, float* LSE,
+                                     void* workspace, size_t workspace_bytes, int P, int S, int H, int H_kv, int N, int d, int prefix_capacity,
+                                     int capacity, int causal, float softmax_scale, void* stream) {
+  bool empty;
+  int st = check_shared(P, S, H, H_kv, N, d, prefix_capacity, capacity, &empty);
+  if (st != ATTN_OK) return st;
+  if (!scale_ok(softmax_scale)) return ATTN_ERR_BAD_ARG;
+  if (empty) return ATTN_OK;
+  if (!Q || !K_prefix || !V_prefix || !K_prefix_scale || !V_prefix_scale || !prefix_lengths || !K_cache || !V_cache || !K_scale || !V_scale ||
+      !lengths || !O || !LSE)
+    return ATTN_ERR_NULL;
+  if (!all_aligned16(Q, K_prefix, V_prefix, K_prefix_scale, V_prefix_scale, K_cache, V_cache, K_scale, V_scale, O, LSE) ||
+      !aligned4(prefix_lengths) || !aligned4(lengths) || !aligned4(counts))
+    return ATTN_ERR_BAD_ARG;
+  for (const void* p : {Q, K_prefix, V_prefix, (const void*)K_prefix_scale, (const void*)V_prefix_scale, K_cache, V_cache, (const void*)K_scale, (const void*)V_scale})
+    if (O == p || LSE == p) return ATTN_ERR_BAD_ARG;
+  if (O == LSE) return ATTN_ERR_BAD_ARG;
+  if (strides && (!strides_ok(strides, 0) || !strides_ok(strides + 3, 1))) return ATTN_ERR_BAD_ARG;
+  const size_t need = attn_cache_fwd_shared_partial_bytes(P, S, H, H_kv, N, d, prefix_capacity, capacity);
+  if (need > 0 && !workspace) return ATTN_ERR_NULL;
+  if (need > 0 && (workspace_bytes < need || !aligned16(workspace))) return ATTN_ERR_WORKSPACE;
+  const Strides q = strides_of(strides, H, N, d), o = strides_of(strides ? strides + 3 : nullptr, H, N, d);
+  using u16 = unsigned short;
+  using u8 = unsigned char;
+  auto cache = [](const void* K, const void* V, const float* Ks, const float* Vs, int tokens) {
+    return CacheArgs{static_cast<u8*>(const_cast<void*>(K)), static_cast<u8*>(const_cast<void*>(V)), const_cast<float*>(Ks), const_cast<float*>(Vs), tokens};
+  };
+  SharedArgs a{};
+  AttendArgs& p = a.own;
+  p.cache = cache(K_cache, V_cache, K_scale, V_scale, capacity);
+  p.Q = Rows{static_cast<const u16*>(Q), q.b, q.h, q.n};
+  p.O = static_cast<u16*>(O);
+  p.o_sb = o.b; p.o_sh = o.h; p.o_sn = o.n;
+  p.LSE = LSE;
+  p.lengths = lengths;
+  p.counts = counts;
+  p.B = P * S; p.H = H; p.H_kv = H_kv; p.N = N; p.group = H / H_kv; p.causal = causal != 0;
+  p.scale = softmax_scale;
+  p.partials = static_cast<float*>(workspace);
+  a.prefix = cache(K_prefix, V_prefix, K_prefix_scale, V_prefix_scale, prefix_capacity);
+  a.prefix_lengths = prefix_lengths;
+  a.P = P; a.S = S;
+  return launched(attn_cache_fwd_shared_dispatch(a, d, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" int attn_cache_fork(const void* K_cache, const void* V_cache, const float* K_scale, const float* V_scale, const int* sources, const int* lengths,
+                               void* K_out, void* V_out, float* K_scale_out, float* V_scale_out, int* lengths_out, int B, int B_out, int H_kv, int d,
+                               int capacity, int capacity_out, void* stream) {
+  bool empty, none;
+  int st = check_rows(B, H_kv, 1, d, &none);
+  if (st != ATTN_OK || (st = check_rows(B_out, H_kv, 1, d, &empty)) != ATTN_OK) return st;
+  if (empty) return ATTN_OK;
+  if (none) return ATTN_ERR_BAD_ARG;       // nothing to copy from
+  if ((st = check_cache(B, H_kv, d, capacity)) != ATTN_OK || (st = check_cache(B_out, H_kv, d, capacity_out)) != ATTN_OK) return st;
+  if (!K_cache || !V_cache || !K_scale || !V_scale || !sources || !lengths || !K_out || !V_out || !K_scale_out || !V_scale_out || !lengths_out)
+    return ATTN_ERR_NULL;
+  if (!all_aligned16(K_cache, V_cache, K_scale, V_scale, K_out, V_out, K_scale_out, V_scale_out) || !aligned4(sources) || !aligned4(lengths) ||
+      !aligned4(lengths_out))
+    return ATTN_ERR_BAD_ARG;
+  const void* ins[] = {K_cache, V_cache, K_scale, V_scale, sources, lengths};
+  const void* outs[] = {K_out, V_out, K_scale_out, V_scale_out, lengths_out};
+  for (int i = 0; i < 5; ++i) {
+    for (const void* p : ins)
+      if (outs[i] == p) return ATTN_ERR_BAD_ARG;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] == outs[j]) return ATTN_ERR_BAD_ARG;
+  }
+  using u8 = unsigned char;
+  ForkArgs a{};
+  a.from = CacheArgs{static_cast<u8*>(const_cast<void*>(K_cache)), static_cast<u8*>(const_cast<void*>(V_cache)),
+                     const_cast<float*>(K_scale), const_cast<float*>(V_scale), capacity};
+  a.to = CacheArgs{static_cast<u8*>(K_out), static_cast<u8*>(V_out), K_scale_out, V_scale_out, capacity_out};
+  a.sources = sources;
+  a.lengths = lengths;
+  a.lengths_out = lengths_out;
+  a.B_in = B; a.B_out = B_out; a.H_kv = H_kv; a.d = d;
+  return launched(attn_cache_fork_dispatch(a, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" int attn_cache_reorder(void* K_cache, void* V_cache, float* K_scale, float* V_scale, const int* parents, const int* lengths, int* lengths_out,
+                                  int P, int S, int H_kv, int d, int capacity, void* stream) {
+  bool empty;
+  if (P < 0 || S < 0) return ATTN_ERR_BAD_ARG;
+  if (S > kMostReordered || P > 65535) return ATTN_ERR_UNSUPPORTED;
+  int st = check_rows(P * S, H_kv, 1, d, &empty);
+  if (st != ATTN_OK) return st;
+  if (empty) return ATTN_OK;
+  if ((st = check_cache(P * S, H_kv, d, capacity)) != ATTN_OK) return st;
+  if (!K_cache || !V_cache || !K_scale || !V_scale || !parents || !lengths || !lengths_out) return ATTN_ERR_NULL;
+  if (!all_aligned16(K_cache, V_cache, K_scale, V_scale) || !aligned4(parents) || !aligned4(lengths) || !aligned4(lengths_out)) return ATTN_ERR_BAD_ARG;
+  const void* all[] = {K_cache, V_cache, K_scale, V_scale, lengths_out, parents, lengths};
+  for (int i = 0; i < 5; ++i)              // (parents and lengths are only read)
+    for (int j = i + 1; j < 7; ++j)
+      if (all[i] == all[j]) return ATTN_ERR_BAD_ARG;
+  using u8 = unsigned char;
+  ReorderArgs a{};
+  a.cache = CacheArgs{static_cast<u8*>(K_cache), static_cast<u8*>(V_cache), K_scale, V_scale, capacity};
+  a.parents = parents;
+  a.lengths = lengths;
+  a.lengths_out = lengths_out;
+  a.P = P; a.S = S; a.H_kv = H_kv; a.d = d;
+  return launched(attn_cache_reorder_dispatch(a, static_cast<hipStream_t>(stream)));
+}
+
+static int check_select(int B, int beams, int V, int n, bool* empty) {
+  *empty = false;
+  if (B < 0 || beams < 0 || V < 0 || n < 0) return ATTN_ERR_BAD_ARG;
+  if (B == 0 || n == 0) { *empty = true; return ATTN_OK; }
+  if (beams < 1 || V < 1) return ATTN_ERR_BAD_ARG;
+  return beams <= kMostBeams && n <= kMostChosen && V <= 1 << 24 && B <= 1 << 20 ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
+}
+
+extern "C" size_t attn_beam_select_workspace_bytes(int B, int beams, int V, int n) {
+  bool empty;
+  return check_select(B, beams, V, n, &empty) != ATTN_OK || empty ? 0 : attn_beam_select_partial_bytes(B, beams, V, n);
+}
+
+extern "C" int attn_beam_select(const void* logits, int logits_type, long long stride_b, long long stride_beam, const float* scores,
+                                const unsigned char* finished, int end_token, int* parents, int* tokens, float* scores_out,
+                                unsigned char* finished_out, void* workspace, size_t workspace_bytes, int B, int beams, int V, int n, void* stream) {
+  bool empty;
+  const int st = check_select(B, beams, V, n, &empty);
+  if (st != ATTN_OK) return st;
+  if (logits_type != ATTN_LOGITS_BF16 && logits_type != ATTN_LOGITS_FLOAT32) return ATTN_ERR_BAD_ARG;
+  if (end_token >= V || (finished && end_token < 0)) return ATTN_ERR_BAD_ARG;
+  if (empty) return ATTN_OK;
+  if (!logits || !scores || !parents || !tokens || !scores_out) return ATTN_ERR_NULL;
+  const bool wide = logits_type == ATTN_LOGITS_FLOAT32;
+  if ((reinterpret_cast<uintptr_t>(logits) & (wide ? 3u : 1u)) != 0 || !aligned4(scores) || !aligned4(parents) || !aligned4(tokens) || !aligned4(scores_out))
+    return ATTN_ERR_BAD_ARG;
+  if (stride_b < 0 || stride_beam < 0 || stride_b >= (1ll << 40) || stride_beam >= (1ll << 40)) return ATTN_ERR_BAD_ARG;
+  const void* ins[] = {logits, scores, finished};
+  const void* outs[] = {parents, tokens, scores_out, finished_out};
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; outs[i] && j < 3 + i; ++j)
+      if (outs[i] == (j < 3 ? ins[j] : outs[j - 3])) return ATTN_ERR_BAD_ARG;
+  if (!workspace) return ATTN_ERR_NULL;
+  if (workspace_bytes < attn_beam_select_partial_bytes(B, beams, V, n) || !aligned16(workspace)) return ATTN_ERR_WORKSPACE;
+  BeamArgs a{};
+  a.logits = logits;
+  a.stride_b = stride_b; a.stride_beam = stride_beam;
+  a.wide = wide;
+  a.scores = scores;
+  a.finished = finished;
+  a.end_token = end_token < 0 ? -1 : end_token;
+  a.parents = parents;
+  a.tokens = tokens;
+  a.scores_out = scores_out;
+  a.finished_out = finished_out;
+  a.B = B; a.beams = beams; a.V = V; a.n = n;
+  a.workspace = workspace;
+  return launched(attn_beam_select_dispatch(a, static_cast<hipStream_t>(stream)));
 }

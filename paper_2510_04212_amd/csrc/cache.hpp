@@ -1,5 +1,5 @@
 // The cache of keys and values in 8 bits (include/attn.h describes it): what its kernels share, and what the entry
-// points (api_cache.hip) hand to them (cache.hip, cache_attn.hip).
+// points (api_cache.hip) hand to them (cache.hip, cache_attn.hip, cache_shared.hip, cache_copy.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -44,6 +44,16 @@ struct AttendArgs {
 size_t attn_cache_fwd_partial_bytes(int B, int H, int H_kv, int N, int d, int capacity);
 hipError_t attn_cache_fwd_dispatch(const AttendArgs&, int d, hipStream_t);
 
+// Sequences that continue prefixes: `own` is about the sequences and their own caches, P * S of them; sequence b continues prefix b / S.
+struct SharedArgs {
+  AttendArgs own;
+  CacheArgs prefix;                        // of P sequences
+  const int* prefix_lengths;
+  int P, S;
+};
+size_t attn_cache_fwd_shared_partial_bytes(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity);
+hipError_t attn_cache_fwd_shared_dispatch(const SharedArgs&, int d, hipStream_t);
+
 struct WeighArgs {
   CacheArgs cache;
   Rows Q;
@@ -65,6 +75,23 @@ struct EvictArgs {
   int B, H_kv, budget, recent;
 };
 hipError_t attn_cache_evict_dispatch(const EvictArgs&, int d, hipStream_t);
+
+struct ForkArgs {
+  CacheArgs from, to;
+  const int *sources, *lengths;            // [B_out]; [B_in]
+  int* lengths_out;                        // [B_out]
+  int B_in, B_out, H_kv, d;
+};
+hipError_t attn_cache_fork_dispatch(const ForkArgs&, hipStream_t);
+
+struct ReorderArgs {
+  CacheArgs cache;
+  const int *parents, *lengths;            // [P][S] each
+  int* lengths_out;
+  int P, S, H_kv, d;
+};
+constexpr int kMostReordered = 64;         // sequences of a group
+hipError_t attn_cache_reorder_dispatch(const ReorderArgs&, hipStream_t);
 
 #ifdef __HIPCC__
 #include "common.hpp"

@@ -1,565 +1,40 @@
 // Attention over the 8-bit cache (attn_cache_fwd of include/attn.h) and the attention weight that each cached token got
 // (attn_cache_weights).
-//
-// Products.  v_mfma_f32_16x16x32_bf16 on codes widened to bf16 in registers: an E4M3 number times a power of two is a bf16 number, and
-// v_cvt_scalef32_pk_bf16_fp8 forms two of them in one instruction, so that scores and outputs need no scale factor of their own.
-// Nothing passes through LDS on the way: the tile is computed transposed, S^T = K Q^T and O^T += V^T P^T, and both
-// operands from the cache are 16 consecutive bytes per lane as they lie in memory (K in rows, V's blocks in columns):
-//   tile i of 16 tokens (i = 0..3) of a block: the lane of row slot r holds token 16 (r / 4) + 4 i + (r % 4), columns 16 g .. + 15 of every 64,
-//   so that S^T leaves lane group g with the 16 consecutive tokens 16 g .. 16 g + 15 of the block, which are the k-slots that V's
-//   16 bytes of column 16 dt + r have: 8 of them make one instruction's, the other 8 the next one's.
-// The row sum adds the float32 probabilities, not the rounded ones that are multiplied with V: LSE is exact to float32, as the weights
-// exp(S - LSE) need it.  P is rounded to bf16 for that product because the matrix unit takes 16-bit operands: O's relative error (root mean square, against
-// 64 bits) is 0.0022, and 0.0017, O's own rounding, with P in float32, which would take a second product of every tile.
-//
-// Rows.  All query heads of a key/value head share its cache: their queries are one list of rows, row = query * group + head of the
-// group, cut into tiles of M = 16 RT 4 / KW rows.  A work-group's four waves take KW shares of the key blocks of 4 / KW row groups.
-#include "cache.hpp"
+#include "cache_attend.hpp"
 #include <algorithm>
 #include <cmath>
 
 namespace {
 
-constexpr int kThreads = 256;
-typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
-
-// d = 32 c + 8 half + ... of the columns: 16-byte chunks serve 64 columns (lane group g: 16 g ..), an 8-byte one the last 32 (8 g ..)
-template <int D> struct Cols {
-  static constexpr int C64 = D / 64;       // whole chunks
-  static constexpr bool ODD = D % 64 != 0;
-};
-
-DEVI bf16x8 widen8(unsigned lo, unsigned hi, float scale) {
-  union { bf16x2 p[4]; bf16x8 v; } u;
-  u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-  u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-  u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-  return u.v;
-}
-
-// Codes of one lane for a block, 16 bytes (or 8: the last 32 columns of d = 32, 96) each: K's of tile i, columns 64 c ..; V's of column tile dt.
-// From memory into registers: every wave reads its own blocks.  K + V: 2 d registers / 8.
-template <int D> struct KCodes {
-  u32x4 c[4][Cols<D>::C64 ? Cols<D>::C64 : 1];
-  u32x2 odd[4];
-  // block: its first byte, the same in all lanes; at: the lane's offset
-  DEVI void load(const unsigned char* block, unsigned at, unsigned at_odd) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int k = 0; k < Cols<D>::C64; ++k) c[i][k] = *reinterpret_cast<const u32x4*>(block + at + (i * 4 * D + k * 64));
-      if constexpr (Cols<D>::ODD) odd[i] = *reinterpret_cast<const u32x2*>(block + at_odd + (i * 4 * D + Cols<D>::C64 * 64));
-    }
-  }
-};
-template <int D> struct VCodes {
-  u32x4 c[D / 16];
-  DEVI void load(const unsigned char* block, unsigned at) {
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) c[dt] = *reinterpret_cast<const u32x4*>(block + at + dt * 1024);
-  }
-};
-// From LDS, where a block's codes are shared by the four waves of a work-group.  Pieces of 1 KB, one transfer instruction each: 16 rows (tokens of
-// a tile, or columns of V) x 64 bytes, the four 16-byte chunks of row r permuted by slot_mask(r / 4) (common.hpp: 16 lanes reading
-// chunk g of 16 rows then meet all banks once); two tiles' 32 bytes a row for the last columns of d = 32, 96.
-template <int D> struct Staged {
-  static constexpr int KP = 4 * Cols<D>::C64 + (Cols<D>::ODD ? 2 : 0), PIECES = KP + D / 16;
-  static constexpr int kBytes = PIECES * 1024;
-  // the byte of the block that lane `lane` of piece i fetches, K's (i < KP) and V's
-  static DEVI unsigned source(int i, int lane) {
-    if (i < 4 * Cols<D>::C64) {
-      const int r = lane >> 2, tile = i / (Cols<D>::C64 ? Cols<D>::C64 : 1), c = i % (Cols<D>::C64 ? Cols<D>::C64 : 1);
-      return (unsigned)(((r >> 2) * 16 + tile * 4 + (r & 3)) * D + c * 64 + (((lane & 3) ^ slot_mask(r >> 2)) << 4));
-    }
-    if (i < KP) {
-      const int r = (lane >> 1) & 15, tile = 2 * (i - 4 * Cols<D>::C64) + (lane >> 5);
-      return (unsigned)(((r >> 2) * 16 + tile * 4 + (r & 3)) * D + Cols<D>::C64 * 64 + ((lane & 1) << 4));
-    }
-    const int r = lane >> 2;
-    return (unsigned)(((i - KP) * 16 + r) * kBlock + (((lane & 3) ^ slot_mask(r >> 2)) << 4));
-  }
-};
-typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
-typedef __attribute__((address_space(3))) const u32x2 lds_u32x2;
-// at, at_odd: LDS addresses, the buffer's + the lane's
-template <int D> DEVI void read_staged(KCodes<D>& k, int at, int at_odd) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int c = 0; c < Cols<D>::C64; ++c) k.c[i][c] = *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (i * Cols<D>::C64 + c) * 1024));
-    if constexpr (Cols<D>::ODD) k.odd[i] = *reinterpret_cast<lds_u32x2*>((unsigned long)(unsigned)(at_odd + 4 * Cols<D>::C64 * 1024 + i * 512));
-  }
-}
-template <int D> DEVI void read_staged(VCodes<D>& v, int at) {
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) v.c[dt] = *reinterpret_cast<lds_u32x4*>((unsigned long)(unsigned)(at + (Staged<D>::KP + dt) * 1024));
-}
-// 64 lanes' 16 bytes each from block + at into LDS at `to` .. + 1023; `block` and `to` the same in all lanes.  Inline assembly as in common.hpp's
-// TileLoader, and for its reasons; waited for with wait_vmem().
-DEVI void fetch_piece(const unsigned char* block, unsigned at, unsigned to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(at), "s"(block) : "m0");
-}
-DEVI bf16x8 key_frag(const u32x4& w, int half, float scale) { return widen8(w[2 * half], w[2 * half + 1], scale); }
-
-// the columns of a query row that go with fragment k: 8 consecutive from here
-template <int D> DEVI int query_column(int k, int g) {
-  return k < 2 * Cols<D>::C64 ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : Cols<D>::C64 * 64 + g * 8;
-}
-
-DEVI float max_over_groups(float x) {
-  unsigned u = __float_as_uint(x);
-  auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  u = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-DEVI int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// ---- The list of segments (cache_shares.hpp): every thread sums up the units of a run of (sequence, tile) items, for one head; a scan over the threads.
-struct Runs {
-  int before[kThreads + 1];                // units in front of thread t's run
-  int waves[kThreads / 64];
-  Segment segment;
-};
-// units of all items
-DEVI int scan_units(const Problem& q, int items, int run, Runs& runs) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int x = 0;
-  for (int i = tid * run; i < min(items, (tid + 1) * run); ++i) x += q.cost(i / q.tiles, i % q.tiles);
-  x = (int)sum_to_lane((unsigned)x);
-  if (lane == 63) runs.waves[wave] = x;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kThreads / 64 - 1; ++w) x += w < wave ? runs.waves[w] : 0;
-  runs.before[tid + 1] = x;
-  if (tid == 0) runs.before[0] = 0;
-  __syncthreads();
-  return uniform(runs.before[kThreads]);
-}
-// The segment of unit `pos`, found by the thread whose run holds it.
-DEVI Segment find_segment(const Problem& q, int B, int H_kv, int run, int pos, Runs& runs) {
-  auto units_before = [&](int item) {      // in front of an item
-    int x = runs.before[item / run];
-    for (int i = item / run * run; i < item; ++i) x += q.cost(i / q.tiles, i % q.tiles);
-    return x;
-  };
-  const int tid = threadIdx.x;
-  int b = -1, first = 0, each = 0, here = runs.before[tid];
-  for (int i = tid * run; i < min(B * q.tiles, (tid + 1) * run); ++i) {
-    if (i / q.tiles != b) {
-      b = i / q.tiles;
-      first = units_before(b * q.tiles);
-      each = units_before((b + 1) * q.tiles) - first;
-    }
-    Segment s;
-    if (locate(q, b, i % q.tiles, first, each, here - first, H_kv, pos, &s)) runs.segment = s;
-    here += q.cost(b, i % q.tiles);
-  }
-  __syncthreads();
-  Segment s = runs.segment;
-  s.b = uniform(s.b);
-  s.h = uniform(s.h);
-  s.t = uniform(s.t);
-  s.begin = uniform(s.begin);
-  return s;
-}
-
-// ---- state of a wave's rows: lane (r, g) has row r of each of its RT tiles, output columns 16 dt + 4 g .. + 3
-template <int D, int RT> struct Acc {
-  f32x4 o[RT][D / 16];
-  float l[RT];                    // sum of the probabilities of the lane's own tokens (of all four groups' after join_groups)
-  float m[RT];                    // running maximum of the scores, in units of log 2; the same in the four groups
-  DEVI void clear() {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      m[rt] = -INFINITY;
-      l[rt] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) o[rt][dt] = f32x4{0, 0, 0, 0};
-    }
-  }
-  DEVI void join_groups() {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) l[rt] = sum_over_groups(l[rt]);
-  }
-  DEVI void scale(int rt, float by) {
-    l[rt] *= by;
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) o[rt][dt] *= by;
-  }
-};
-template <int D, int RT, int KW> constexpr int kSlotFloats = (4 / KW) * RT * (D / 16 * 256 + 32);
-
-// A row of the list: which query and head it is, and how many tokens it sees.
-struct Row {
-  int query, head, limit;
-  bool there, empty;                    // empty: its output is 0
-};
-DEVI Row find_row(const AttendArgs& p, int b, int row) {
-  const int n = real_count(p.counts, b, p.N);
-  const long long length = p.lengths[b];
-  const long long all = max(0ll, min(length, (long long)p.cache.capacity));
-  Row x;
-  x.there = row < p.N * p.group;
-  x.query = x.there ? row / p.group : 0;
-  x.head = x.there ? row - x.query * p.group : 0;
-  const long long seen = p.causal ? min(all, length - n + x.query + 1) : all;
-  x.empty = x.query >= n || seen <= 0;
-  x.limit = x.there && x.query < n ? (int)max(0ll, seen) : 0x7fffffff;       // a row that nobody asks for needs no masking
-  return x;
-}
-// O and LSE of a row: DT column tiles from dt0 on
-template <int DT>
-DEVI void store_row(const AttendArgs& p, const Row& x, int b, int h, const f32x4* o, float m, float l, int dt0, int g) {
-  if (!x.there) return;
-  const int head = h * p.group + x.head;
-  unsigned short* to = p.O + b * p.o_sb + head * p.o_sh + x.query * p.o_sn + dt0 * 16 + g * 4;
-  const Divisor by = make_divisor(l);
-#pragma unroll
-  for (int i = 0; i < DT; ++i) {
-    union { bf16x4 v; u32x2 w; } u;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) u.v[c] = x.empty ? (bf16_t)0.f : (bf16_t)divide(o[i][c], by);
-    *reinterpret_cast<u32x2*>(to + i * 16) = u.w;
-  }
-  if (dt0 == 0 && g == 0) p.LSE[((size_t)b * p.H + head) * p.N + x.query] = x.empty ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-}
-
-// bytes of w that are 0x7f or 0xff, E4M3's NaN: 0x80 in each of them
-DEVI unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-
-// A masked block whose V holds NaN: 0 * NaN must not reach the rows that do not see that token.  The codes are made 0, and an
-// output to which a row's visible tokens bring a NaN is made one: that count is a product, too, of ones.
-template <int D, int RT>
-DEVI void take_out_nan(Acc<D, RT>& a, VCodes<D>& v, const int (&limit)[RT], int t0, int g) {
-  int seen[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    seen[rt] = limit[rt] - t0 - 16 * g;
-    settle(seen[rt]);                      // (a copy: or the masks are formed for both uses at once, and kept)
-  }
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const unsigned lo = nan_codes(v.c[dt][2 * j]), hi = nan_codes(v.c[dt][2 * j + 1]);
-      v.c[dt][2 * j] &= ~((lo >> 7) * 0xffu);
-      v.c[dt][2 * j + 1] &= ~((hi >> 7) * 0xffu);
-      bf16x8 ones;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)((((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0x80u) ? 1.f : 0.f);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        bf16x8 sees;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sees[e] = (bf16_t)(8 * j + e < seen[rt] ? 1.f : 0.f);
-        const f32x4 count = mfma16(ones, sees, f32x4{0, 0, 0, 0});
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (count[i] > 0.f) a.o[rt][dt][i] = NAN;
-      }
-    }
-}
-
-// One block of 64 tokens for a wave's rows.  masked (the same in all lanes): some row does not see all of it.  after_scores() is called when
-// K's codes have been used.
-//
-// The maximum that probabilities are taken relative to is let fall behind the true one by up to kSlack (a factor of 2^kSlack, harmless in float32 and
-// bf16 alike), so that the accumulators are hardly ever rescaled.
-//
-// Of the two waves that share a SIMD, the one that multiplies goes first, so that the other's softmax fills in (2048 queries over 16384 tokens, H 32/8,
-// d 128: 534 -> 493 us; 16 queries of 64 sequences of 4300: 126 -> 121; d = 64, 4096 queries of 4 sequences: 441 -> 413; with one wave a SIMD, d = 256, even:
-// not there).
-constexpr float kSlack = 8.f;
-template <int D, int RT, class F>
-DEVI void block_step(Acc<D, RT>& a, const bf16x8 (&q)[RT][D / 32], const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, float scale_log2,
-                     const int (&limit)[RT], bool masked, int t0, int g, F&& after_scores) {
-  constexpr bool kMultipliesFirst = D < 256;
-  f32x4 s[RT][4];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[rt][i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int c = 0; c < Cols<D>::C64; ++c) {
-      const u32x4 w = k.c[i][c];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const bf16x8 kf = key_frag(w, half, k_scale);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][2 * c + half], s[rt][i]);
-      }
-    }
-    if constexpr (Cols<D>::ODD) {
-      const u32x2 w = k.odd[i];
-      const bf16x8 kf = widen8(w.x, w.y, k_scale);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s[rt][i] = mfma16(kf, q[rt][D / 32 - 1], s[rt][i]);
-    }
-  }
-  if (kMultipliesFirst) __builtin_amdgcn_s_setprio(0);
-  after_scores();
-  if (masked) {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int seen = limit[rt] - t0 - 16 * g;
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i >= seen) s[rt][i / 4][i % 4] = -INFINITY;
-    }
-    if (v_scale < 0.f) take_out_nan<D, RT>(a, v, limit, t0, g);          // V's scale is negative: a code of the block is NaN
-  }
-  v_scale = __builtin_fabsf(v_scale);
-  bf16x8 pr[RT][2];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    float most = s[rt][0][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[rt][i / 4][i % 4]);
-    most = max_over_groups(most) * scale_log2;
-    if (__any(most > a.m[rt] + kSlack)) {
-      const float m = most > a.m[rt] + kSlack ? most : a.m[rt];
-      a.scale(rt, __builtin_amdgcn_exp2f(a.m[rt] - (m == -INFINITY ? 0.f : m)));
-      a.m[rt] = m;
-    }
-    const float use = a.m[rt] == -INFINITY ? 0.f : a.m[rt];            // nothing seen so far: exp2(-inf) = 0
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][2 * j + e / 4][e % 4], scale_log2, -use));
-        a.l[rt] += x;
-        pr[rt][j][e] = (bf16_t)x;
-      }
-  }
-  if (kMultipliesFirst) __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) {
-    const u32x4 w = v.c[dt];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bf16x8 vf = widen8(w[2 * j], w[2 * j + 1], v_scale);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) a.o[rt][dt] = mfma16(vf, pr[rt][j], a.o[rt][dt]);
-    }
-  }
-}
+constexpr int kThreads = kAttendThreads;
 
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
-//
-// KW = 4, few rows: bound by bytes; every wave reads blocks of its own straight into registers, K's a block ahead (one token of 64 sequences of 4300, H 32/8, d
-// 128: 100 us, 5.6 TB/s).  KW = 1, many rows: bound by
-// the vector and matrix units; the four waves share a block through LDS, filled by asynchronous transfers a block ahead (three blocks ahead, in four
-// buffers: 16 queries of 64 sequences of 4300 tokens, H 32/8, d 128, 139 us; one ahead, in two: 125.  2048 queries over 16384: 636 and 620; these with the
-// loop of that time, which takes 121 and 493 now).
 template <int D, int RT, int KW, bool SPLIT>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
-  constexpr int RG = 4 / KW, M = 16 * RT * RG;
-  static_assert(KW == 1 || KW == 4, "the four waves have rows of their own, or blocks");
   __shared__ Runs runs;
-  __shared__ f32x4 joined[KW == 4 ? 4 * RT * (D / 16) * 64 : 1];         // [wave][RT][D / 16][lane]
-  __shared__ float joined_m[KW == 4 ? 4 * RT * 16 : 1], joined_l[KW == 4 ? 4 * RT * 16 : 1];
-  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? 2 * Staged<D>::kBytes : 16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int r = lane & 15, g = lane >> 4;
-  const int kw = wave % KW, rg = wave / KW;
-  const Problem q{p.lengths, p.counts, p.cache.capacity, p.N, p.group, p.causal, tiles, M};
-  const int nb = p.cache.capacity / kBlock;
-  const float scale_log2 = p.scale * kLog2e;
-
-  Segment seg;
-  int pos, end, w = 0;
-  Shares all{1, 0, 0};
-  Join* notes = reinterpret_cast<Join*>(p.partials);
+  const Problem q{p.lengths, p.counts, p.cache.capacity, p.N, p.group, p.causal, tiles, 16 * RT * 4 / KW};
+  const PlainCall call{p};
+  Work work{{}, 0, 0, 0, {1, 0, 0}};
+  Parts parts{reinterpret_cast<Join*>(p.partials), p.partials + most_shares * (sizeof(Join) / sizeof(float)), notes_by_segment};
   if constexpr (SPLIT) {
     const int items = p.B * tiles, run = (items + kThreads - 1) / kThreads;
-    all = shares_of(p.H_kv * scan_units(q, items, run, runs), most_shares, kLeastUnits<KW>);
-    w = share_of(blockIdx.x, all.number);
-    if (w < 0) return;
-    pos = uniform(all.begin(w));
-    end = uniform(all.begin(w + 1));
-    seg = find_segment(q, p.B, p.H_kv, run, pos, runs);
-    if (tid == 0 && !notes_by_segment) notes[w] = note_of_share(all, w, seg, p.H_kv, tiles);
+    work.all = shares_of(p.H_kv * scan_units(q, items, run, runs), most_shares, kLeastUnits<KW>);
+    work.w = share_of(blockIdx.x, work.all.number);
+    if (work.w < 0) return;
+    work.pos = uniform(work.all.begin(work.w));
+    work.end = uniform(work.all.begin(work.w + 1));
+    work.seg = find_segment(q, p.B, p.H_kv, run, work.pos, runs);
+    if (threadIdx.x == 0 && !notes_by_segment) parts.notes[work.w] = note_of_share(work.all, work.w, work.seg, p.H_kv, tiles);
   } else {
-    seg.b = blockIdx.z;
-    seg.h = blockIdx.x;
-    seg.t = blockIdx.y;
-    seg.begin = 0;
-    seg.blocks = q.blocks(seg.b, seg.t);
-    pos = 0;
-    end = seg.end();
+    work.seg.b = blockIdx.z;
+    work.seg.h = blockIdx.x;
+    work.seg.t = blockIdx.y;
+    work.seg.begin = 0;
+    work.seg.blocks = q.blocks(work.seg.b, work.seg.t);
+    work.end = work.seg.end();
   }
-  seg.blocks = uniform(seg.blocks);
-
-  while (true) {
-    const int to = min(end, seg.end());
-    if (SPLIT && notes_by_segment && tid == 0 && pos == seg.begin)
-      notes[segment_number(seg, p.H_kv, tiles)] = note_of_segment(all, w, seg, p.H_kv, tiles);
-    const int b = seg.b, h = seg.h, first_row = seg.t * M + rg * RT * 16;
-    const int blk0 = seg.block_at(pos), blk_end = seg.block_at(to);
-    const size_t bh = (size_t)b * p.H_kv + h;
-    const unsigned char* K = p.cache.K + bh * p.cache.capacity * D;
-    const unsigned char* V = p.cache.V + bh * p.cache.capacity * D;
-    const float* Ks = p.cache.K_scale + bh * nb;
-    const float* Vs = p.cache.V_scale + bh * nb;
-    // a wave of few rows: its first block is on its way while the queries are looked for
-    const unsigned at = ((r >> 2) * 16 + (r & 3)) * D + g * 16, at_odd = ((r >> 2) * 16 + (r & 3)) * D + g * 8, at_v = r * kBlock + g * 16;
-    KCodes<D> k;
-    float k_scale = 0.f, next_v = 0.f;     // loaded with K's codes: a load behind V's would have V waited for
-    auto load_key = [&](int blk) {
-      if (blk >= blk_end) return;
-      k_scale = Ks[blk];
-      next_v = Vs[blk];
-      k.load(K + (size_t)blk * (kBlock * D), at, at_odd);
-    };
-    if constexpr (KW == 4) load_key(blk0 + kw);
-    int least = 0x7fffffff, limit[RT];
-    bf16x8 qf[RT][D / 32];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const Row x = find_row(p, b, first_row + rt * 16 + r);
-      limit[rt] = x.limit;
-      least = min(least, x.limit);
-      const unsigned short* from = p.Q.at + b * p.Q.sb + (h * p.group + x.head) * p.Q.sh + x.query * p.Q.sn;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) qf[rt][c] = *reinterpret_cast<const bf16x8*>(from + query_column<D>(c, g));
-    }
-#pragma unroll
-    for (int i = 1; i < 16; i <<= 1) least = min(least, __shfl_xor(least, i));
-    least = uniform(least);
-
-    Acc<D, RT> a;
-    a.clear();
-    if constexpr (KW == 1) {
-      // a wave fetches every fourth piece; PIECES is a multiple of 4
-      constexpr int MINE = Staged<D>::PIECES / 4;
-      const unsigned buffers = uniform(lds_address(staged));
-      unsigned from[MINE];
-#pragma unroll
-      for (int i = 0; i < MINE; ++i) from[i] = Staged<D>::source(wave + 4 * i, lane);
-      auto fetch = [&](int blk, int buffer) {
-#pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-          const int piece = wave + 4 * i;
-          fetch_piece((piece < Staged<D>::KP ? K : V) + (size_t)blk * (kBlock * D), from[i], buffers + buffer * Staged<D>::kBytes + piece * 1024);
-        }
-      };
-      const int in_piece = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), in_odd = r * 32 + g * 8;
-      const bool rows_here = first_row < p.N * p.group;
-      // Scales: 64 blocks' at a time, one in each lane.
-      float k_scales = 0.f, v_scales = 0.f;
-      auto load_scales = [&](int blk) {
-        const int mine = min(blk + lane, nb - 1);
-        k_scales = Ks[mine];
-        v_scales = Vs[mine];
-        settle(k_scales);
-        settle(v_scales);
-      };
-      __syncthreads();                                     // nobody reads the last segment's blocks any more
-      if (blk0 < blk_end) {
-        fetch(blk0, 0);
-        load_scales(blk0);
-      }
-      // What the compiler has loaded is settled here: waits that it placed inside the loop, where it knows nothing of the transfers, would wait for these.
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) settle(qf[rt][c]);
-      int buffer = 0;
-      for (int blk = blk0; blk < blk_end; ++blk) {
-        wait_vmem();
-        __syncthreads();                                   // this block has landed for all waves, and all have read the one before
-        if (blk + 1 < blk_end) fetch(blk + 1, buffer ^ 1);
-        if (rows_here) {
-          if (blk > blk0 && ((blk - blk0) & 63) == 0) load_scales(blk);
-          const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), (blk - blk0) & 63));
-          const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), (blk - blk0) & 63));
-          const int base = (int)buffers + buffer * Staged<D>::kBytes;
-          VCodes<D> v;
-          read_staged<D>(k, base + in_piece, base + in_odd);
-          block_step<D, RT>(a, qf, k, v, ks, vs, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g,
-                            [&] { read_staged<D>(v, base + in_piece); });
-        }
-        buffer ^= 1;
-      }
-    } else {
-      for (int blk = blk0 + kw; blk < blk_end; blk += KW) {
-        VCodes<D> v;
-        v.load(V + (size_t)blk * (kBlock * D), at_v);
-        block_step<D, RT>(a, qf, k, v, k_scale, next_v, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g,
-                          [&] { load_key(blk + KW); });
-      }
-    }
-
-    a.join_groups();
-    const bool whole = !SPLIT || (pos == seg.begin && to == seg.end());
-    float* slot = p.partials + most_shares * (sizeof(Join) / sizeof(float)) + (size_t)(2 * w + (pos == seg.begin ? 1 : 0)) * kSlotFloats<D, RT, KW>;
-    // O and LSE of a finished row, or this part of them: column tiles dt0 .. dt0 + DT - 1 of row tile `tile`
-    auto put = [&](auto DT, int tile, const f32x4* o, float m, float l, int dt0) {
-      if (whole) {
-        store_row<DT>(p, find_row(p, b, seg.t * M + tile * 16 + r), b, h, o, m, l, dt0, g);
-        return;
-      }
-#pragma unroll
-      for (int i = 0; i < DT; ++i) reinterpret_cast<f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + lane] = o[i];
-      float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;
-      if (g == 0 && dt0 == 0) {
-        ml[r] = m;
-        ml[16 + r] = l;
-      }
-    };
-    if constexpr (KW == 1) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) put(std::integral_constant<int, D / 16>{}, rg * RT + rt, a.o[rt], a.m[rt], a.l[rt], 0);
-    } else {
-      // Four waves have four sums of the same rows: all go to LDS as they are, and each wave joins RT * D / 64 of the RT * D / 16 tiles
-      // (d = 32: the first two).
-      __syncthreads();                                     // the last segment's have been read
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) joined[((wave * RT + rt) * (D / 16) + dt) * 64 + lane] = a.o[rt][dt];
-        if (g == 0) {
-          joined_m[(wave * RT + rt) * 16 + r] = a.m[rt];
-          joined_l[(wave * RT + rt) * 16 + r] = a.l[rt];
-        }
-      }
-      __syncthreads();
-      constexpr int EACH = D / 16 >= 4 ? D / 16 / 4 : 1, REST = D / 16 - 4 * EACH;       // column tiles per wave (d = 96: 1, and 2 that are left)
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float by[4], m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) m = fmaxf(m, joined_m[(x * RT + rt) * 16 + r]);
-        const float use = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          by[x] = __builtin_amdgcn_exp2f(joined_m[(x * RT + rt) * 16 + r] - use);
-          l += joined_l[(x * RT + rt) * 16 + r] * by[x];
-        }
-        auto join = [&](auto DT, int dt0) {
-          f32x4 o[DT];
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            o[i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int x = 0; x < 4; ++x) o[i] += joined[((x * RT + rt) * (D / 16) + dt0 + i) * 64 + lane] * by[x];
-          }
-          put(DT, rt, o, m, l, dt0);
-        };
-        if (wave * EACH < D / 16) join(std::integral_constant<int, EACH>{}, wave * EACH);
-        if (REST > 0 && wave < REST) join(std::integral_constant<int, 1>{}, 4 * EACH + wave);
-      }
-    }
-    if constexpr (!SPLIT) break;
-    pos = to;
-    if (pos >= end) break;
-    next_segment(q, p.H_kv, seg);
-    seg.blocks = uniform(seg.blocks);
-  }
+  work.seg.blocks = uniform(work.seg.blocks);
+  attend<D, RT, KW, SPLIT>(call, q, work, parts);
 }
 
 // Joins the parts of the segments that were split between shares.  blockIdx.x is a note; blockIdx.y one row tile of 16 and DT of the D / 16 column
