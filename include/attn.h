@@ -463,7 +463,7 @@ int attn_cache_evict(const void* K_cache, const void* V_cache, const float* K_sc
  *   K_prefix, V_prefix, K_prefix_scale, V_prefix_scale   a cache of P sequences, of prefix_capacity tokens each
  *   prefix_lengths  int32 [P], device
  * Everything else is as in attn_cache_fwd: rounding, statistics and sums, what sees nothing, NaN among values, determinism.
- * ATTN_ERR_UNSUPPORTED also where P * S > 65535, N * H * S >= 2^30, P * S * H_kv * T * ((prefix_capacity + capacity) / 64 + 5) >= 2^30 or T > 65535, with T of
+ * ATTN_ERR_UNSUPPORTED also where P * S > 65535, N * H * S >= 2^30, P * S * H_kv * T * ((prefix_capacity + capacity) / 64 + 10) >= 2^30 or T > 65535, with T of
  * attn_cache_fwd.
  */
 size_t attn_cache_fwd_shared_workspace_bytes(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity);

@@ -278,7 +278,7 @@ static int check_shared(int P, int S, int H, int H_kv, int N, int d, int prefix_
   if ((st = check_cache(P, H_kv, d, prefix_capacity)) != ATTN_OK) return st;
   if ((double)N * H * S >= 1073741824.0) return ATTN_ERR_UNSUPPORTED;      // rows of a prefix: counted in int
   const CacheForm f = cache_form(P * S, H, H_kv, N, d, capacity);
-  const double units = cache_units(P * S, H_kv, f, capacity) + (double)P * S * H_kv * f.tiles * (prefix_capacity / kBlock);
+  const double units = cache_units(P * S, H_kv, f, capacity) + (double)P * S * H_kv * f.tiles * (kStart + prefix_capacity / kBlock);
   return f.tiles <= 65535 && units < kUnitLimit ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
 }
 

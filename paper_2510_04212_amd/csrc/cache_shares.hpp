@@ -156,12 +156,15 @@ inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
 //     8192: 32 91 / 115 full, 61 / 61 ragged, 51 / 35 with one sequence in eight full.  d = 64, 4096: 4 12.1 / 15.3, 24 16.9 / 24.2
 //   more rows, shared blocks: 16, 32 where there is a segment for every work-group that runs at once.  64 rows: 1024: 1 19 / 23;  2048: 4 33 / 24, 64 59 / 63;
 //     4096: 4 61 / 28.  2048 queries of 2048 tokens 65 / 71, 4096 of 4096 197 / 175.
-inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
-  const long long rows = (long long)N * (H / H_kv);
-  CacheForm f;
+inline CacheForm row_form(long long rows) {
+  CacheForm f{};
   f.RT = rows <= 64 ? 1 : 2;
   f.KW = rows <= 16 ? 4 : 1;
   f.tiles = (int)((rows + f.rows() - 1) / f.rows());
+  return f;
+}
+inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
+  CacheForm f = row_form((long long)N * (H / H_kv));
   const double most_shares = cache_units(B, H_kv, f, capacity) / (f.KW == 4 ? kLeastUnits<4> : kLeastUnits<1>);
   const int most = d == 256 ? 256 : 512;   // as many as run at once
   const double segments = (double)B * H_kv * f.tiles;
