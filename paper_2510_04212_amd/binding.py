@@ -812,6 +812,10 @@ def attn_cache_fwd_shared(Q, prefix, prefix_lengths, cache, lengths, softmax_sca
     what attn_cache_fwd says; a prefix is read once for all its sequences.
 
     Everything else is as in attn_cache_fwd; the workspace has cache_fwd_shared_workspace_bytes(...) bytes."""
+    if O is None and LSE is None and workspace is None and stream is None:
+        out = _operators.cache_fwd_shared(*prefix, prefix_lengths, *cache, Q, lengths, softmax_scale, causal, counts)
+        if out is not None:
+            return out
     B, H, H_kv, N, d, capacity, device = _queries(Q, cache)
     P, Hp, prefix_capacity, dp, device_p = _cache_shape(prefix, "prefix")
     if (Hp, dp, device_p) != (H_kv, d, device) or (P == 0) != (B == 0) or (P and B % P):
@@ -841,6 +845,10 @@ def attn_cache_fork(cache, sources, lengths, out=None, stream=None):
     the sequences that have ended, a cache of another capacity.
 
     out: another Cache of len(sources) sequences; a new one of the same capacity when absent."""
+    if stream is None and out is not None:
+        lengths_out = _operators.cache_fork(*cache, sources, lengths, *out)
+        if lengths_out is not None:
+            return out, lengths_out
     B, H_kv, capacity, d, device = _cache_shape(cache)
     _dense(lengths, "lengths", (B,), torch.int32, device)
     if sources.dim() != 1:
@@ -862,6 +870,10 @@ def attn_cache_reorder(cache, parents, lengths, stream=None):
     """lengths_out: int32 [P * S], after the sequences of `cache` have been replaced, in place, by others of their group of S: sequence g * S + s by
     what g * S + parents[g, s] was (int32 [P,S], S <= 64), as attn_beam_select's parents say it.  Values outside 0 .. S - 1 leave a sequence
     as it is; lengths: int32 [P * S]."""
+    if stream is None:
+        lengths_out = _operators.cache_reorder(*cache, parents, lengths)
+        if lengths_out is not None:
+            return lengths_out
     B, H_kv, capacity, d, device = _cache_shape(cache)
     if parents.dim() != 2 or parents.numel() != B:
         raise ValueError("parents must be an int32 tensor [P,S] with a value for each sequence of the cache")
@@ -888,6 +900,10 @@ def attn_beam_select(logits, scores, n, finished=None, end_token=None, workspace
     have ended: they continue with end_token alone, which adds nothing to their score.  ended: whether a continuation is, or had come to, an end.
     Logits of -infinity are never chosen; a beam with a NaN or +infinity, or whose score is not finite, has no continuation.  Where there are fewer
     than n, the rest of parents and tokens is -1, and of the sums -infinity."""
+    if workspace is None and stream is None:
+        out = _operators.beam_select(logits, scores, n, finished, end_token)
+        if out is not None:
+            return out
     if logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda or logits.dim() != 3 or (logits.stride(2) != 1 and logits.shape[2] > 1):
         raise ValueError("logits must be a CUDA float32 or bfloat16 tensor [B,beams,V] whose last dimension is contiguous")
     device = logits.device

@@ -1,4 +1,4 @@
-// Plain calls of the rotary positions and of the 8-bit cache, marshalled in C++ (host code only; every computation is behind the C ABI).
+// Plain calls of the rotary positions, of the 8-bit cache and of the choice among beams, marshalled in C++ (host code only; every computation is behind the C ABI).
 //
 // What bounds a token's step is the host: rotating, appending or attending for one token takes the GPU 4 to 7 us, and the checks, ctypes
 // conversions and allocations of binding.py took longer.  us a call among others, in Python -> here: rotating one token of 32 sequences
@@ -180,6 +180,84 @@ std::optional<std::tuple<Tensor, Tensor>> cache_evict(const Tensor& K, const Ten
   return std::make_tuple(w, kept);
 }
 
+std::optional<std::tuple<Tensor, Tensor>> cache_fwd_shared(const Tensor& Kp, const Tensor& Vp, const Tensor& Kps, const Tensor& Vps, const Tensor& prefix_lengths,
+                                                           const Tensor& K, const Tensor& V, const Tensor& K_scale, const Tensor& V_scale, const Tensor& q,
+                                                           const Tensor& lengths, double scale, bool causal, const OptTensor& counts) {
+  if (!q.defined() || !q.is_cuda()) return std::nullopt;
+  const auto device = c10::hip::current_device();
+  Cache p{Kp, Vp, Kps, Vps}, c{K, V, K_scale, V_scale};
+  if (!c.fits(device) || !p.fits(device) || p.H != c.H || p.d != c.d || c.B % p.B != 0) return std::nullopt;
+  if (!rows(q, device) || q.size(0) != c.B || q.size(3) != c.d || !lengths_fit(lengths, counts, device, c.B) ||
+      !lengths_fit(prefix_lengths, std::nullopt, device, p.B))
+    return std::nullopt;
+  const int P = (int)p.B, S = (int)(c.B / p.B), H = (int)q.size(1), N = (int)q.size(2), d = (int)c.d;
+  const size_t need = attn_cache_fwd_shared_workspace_bytes(P, S, H, (int)c.H, N, d, (int)p.capacity, (int)c.capacity);
+  Tensor o = at::empty({c.B, H, N, d}, q.options());
+  Tensor lse = at::empty({c.B, H, N}, q.options().dtype(at::kFloat));
+  Tensor ws;
+  if (need > 0) ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+  long long strides[6];
+  put(strides, q);
+  put(strides + 3, o);
+  if (!done(attn_cache_fwd_shared(q.data_ptr(), strides, Kp.data_ptr(), Vp.data_ptr(), p.ks(), p.vs(), ints(prefix_lengths), K.data_ptr(), V.data_ptr(), c.ks(),
+                                  c.vs(), ints(lengths), ints(counts), o.data_ptr(), static_cast<float*>(lse.data_ptr()), need > 0 ? ws.data_ptr() : nullptr,
+                                  need, P, S, H, (int)c.H, N, d, (int)p.capacity, (int)c.capacity, causal, (float)scale, stream_of(device))))
+    return std::nullopt;
+  return std::make_tuple(o, lse);
+}
+
+// Into the given cache; its lengths.
+OptTensor cache_fork(const Tensor& K, const Tensor& V, const Tensor& K_scale, const Tensor& V_scale, const Tensor& sources, const Tensor& lengths,
+                     const Tensor& Ko, const Tensor& Vo, const Tensor& Kso, const Tensor& Vso) {
+  if (!K.defined() || !K.is_cuda()) return std::nullopt;
+  const auto device = c10::hip::current_device();
+  Cache c{K, V, K_scale, V_scale}, o{Ko, Vo, Kso, Vso};
+  if (!c.fits(device) || !o.fits(device) || o.H != c.H || o.d != c.d) return std::nullopt;
+  if (!lengths_fit(lengths, std::nullopt, device, c.B) || !lengths_fit(sources, std::nullopt, device, o.B)) return std::nullopt;
+  Tensor left = at::empty({o.B}, lengths.options());
+  if (!done(attn_cache_fork(K.data_ptr(), V.data_ptr(), c.ks(), c.vs(), ints(sources), ints(lengths), Ko.data_ptr(), Vo.data_ptr(), o.ks(), o.vs(),
+                            static_cast<int*>(left.data_ptr()), (int)c.B, (int)o.B, (int)c.H, (int)c.d, (int)c.capacity, (int)o.capacity, stream_of(device))))
+    return std::nullopt;
+  return left;
+}
+
+OptTensor cache_reorder(const Tensor& K, const Tensor& V, const Tensor& K_scale, const Tensor& V_scale, const Tensor& parents, const Tensor& lengths) {
+  if (!K.defined() || !K.is_cuda()) return std::nullopt;
+  const auto device = c10::hip::current_device();
+  Cache c{K, V, K_scale, V_scale};
+  if (!c.fits(device) || !parents.defined() || parents.dim() != 2 || parents.numel() != c.B) return std::nullopt;
+  if (!dense(parents, device, at::kInt, parents.sizes()) || !lengths_fit(lengths, std::nullopt, device, c.B)) return std::nullopt;
+  Tensor left = at::empty({c.B}, lengths.options());
+  if (!done(attn_cache_reorder(K.data_ptr(), V.data_ptr(), c.ks(), c.vs(), ints(parents), ints(lengths), static_cast<int*>(left.data_ptr()),
+                               (int)parents.size(0), (int)parents.size(1), (int)c.H, (int)c.d, (int)c.capacity, stream_of(device))))
+    return std::nullopt;
+  return left;
+}
+
+std::optional<std::tuple<Tensor, Tensor, Tensor, Tensor>> beam_select(const Tensor& logits, const Tensor& scores, int64_t n, const OptTensor& finished,
+                                                                      const std::optional<int64_t>& end_token) {
+  if (!logits.defined() || !logits.is_cuda()) return std::nullopt;
+  const auto device = c10::hip::current_device();
+  const bool wide = logits.scalar_type() == at::kFloat;
+  if (!on(logits, device, wide ? at::kFloat : at::kBFloat16) || logits.dim() != 3 || logits.numel() == 0 || logits.stride(2) != 1) return std::nullopt;
+  const int64_t B = logits.size(0), beams = logits.size(1), V = logits.size(2);
+  if (std::max(std::max(B, beams), V) > INT_MAX || n < 1 || n > INT_MAX || logits.stride(0) < 0 || logits.stride(1) < 0) return std::nullopt;
+  if (!dense(scores, device, at::kFloat, {B, beams}) || (finished && (!end_token || !dense(*finished, device, at::kBool, {B, beams})))) return std::nullopt;
+  if (end_token && (*end_token < 0 || *end_token >= V)) return std::nullopt;
+  const size_t need = attn_beam_select_workspace_bytes((int)B, (int)beams, (int)V, (int)n);
+  if (need == 0) return std::nullopt;      // refused
+  const auto ints_of = logits.options().dtype(at::kInt);
+  Tensor parents = at::empty({B, n}, ints_of), tokens = at::empty({B, n}, ints_of), sums = at::empty({B, n}, scores.options());
+  Tensor ended = at::empty({B, n}, logits.options().dtype(at::kBool)), ws = at::empty({(int64_t)need}, logits.options().dtype(at::kByte));
+  if (!done(attn_beam_select(logits.data_ptr(), wide ? ATTN_LOGITS_FLOAT32 : ATTN_LOGITS_BF16, logits.stride(0), logits.stride(1),
+                             static_cast<const float*>(scores.data_ptr()), finished ? static_cast<const unsigned char*>(finished->data_ptr()) : nullptr,
+                             end_token ? (int)*end_token : -1, static_cast<int*>(parents.data_ptr()), static_cast<int*>(tokens.data_ptr()),
+                             static_cast<float*>(sums.data_ptr()), static_cast<unsigned char*>(ended.data_ptr()), ws.data_ptr(), need, (int)B, (int)beams,
+                             (int)V, (int)n, stream_of(device))))
+    return std::nullopt;
+  return std::make_tuple(parents, tokens, sums, ended);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_operators, m) {
@@ -188,4 +266,8 @@ PYBIND11_MODULE(_operators, m) {
   m.def("cache_fwd", &cache_fwd, "attn_cache_fwd; None: not a plain case");
   m.def("cache_weights", &cache_weights, "attn_cache_weights; None: not a plain case");
   m.def("cache_evict", &cache_evict, "attn_cache_evict; None: not a plain case");
+  m.def("cache_fwd_shared", &cache_fwd_shared, "attn_cache_fwd_shared; None: not a plain case");
+  m.def("cache_fork", &cache_fork, "attn_cache_fork; None: not a plain case");
+  m.def("cache_reorder", &cache_reorder, "attn_cache_reorder; None: not a plain case");
+  m.def("beam_select", &beam_select, "attn_beam_select; None: not a plain case");
 }
