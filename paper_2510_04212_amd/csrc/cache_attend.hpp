@@ -369,7 +369,7 @@ struct Parts {
 
 // What the segments are over: a call's queries and its cache.
 struct PlainCall {
-  static constexpr bool kJoint = false;
+  static constexpr bool kJoint = false, kHeads = false;
   const AttendArgs& p;
   // a row of the list
   DEVI const unsigned short* query(int b, int head, int query) const { return p.Q.at + b * p.Q.sb + head * p.Q.sh + query * p.Q.sn; }
@@ -378,6 +378,10 @@ struct PlainCall {
     store_row<DT>(p, find_row(p, s.b, s.t * M + tile * 16 + (lane & 15)), s.b, s.h, o, m, l, dt0, lane >> 4);
   }
 };
+
+// LDS of a work-group: sums of the four waves to be joined, or two blocks' codes.
+template <int D, int RT, int KW, bool HEADS = false>
+constexpr int kAttendBytes = KW == 4 ? 4 * RT * (D / 16) * 64 * 16 + 2 * 4 * RT * 16 * 4 : HEADS ? 0 : 2 * Staged<D>::kBytes;
 
 // SPLIT: a share of the list of blocks; otherwise one segment, nothing to merge.
 //
@@ -388,18 +392,21 @@ struct PlainCall {
 // loop of that time, which takes 121 and 493 now).
 //
 // Call::kJoint: a segment's blocks are those of its sequence's prefix, then its own.
+// Call::kHeads (KW = 1, few rows): a segment is the same rows of four key/value heads, one for each wave, which reads that head's blocks straight into
+// registers: short segments are begun and ended four at a time, and nothing is joined in LDS.
+// staged: kAttendBytes of LDS, 1 KB aligned.
 template <int D, int RT, int KW, bool SPLIT, class Call>
-DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& parts) {
-  constexpr int RG = 4 / KW, M = 16 * RT * RG;
-  static_assert(KW == 1 || KW == 4, "the four waves have rows of their own, or blocks");
-  __shared__ f32x4 joined[KW == 4 ? 4 * RT * (D / 16) * 64 : 1];         // [wave][RT][D / 16][lane]
-  __shared__ float joined_m[KW == 4 ? 4 * RT * 16 : 1], joined_l[KW == 4 ? 4 * RT * 16 : 1];
-  __shared__ __attribute__((aligned(1024))) char staged[KW == 1 ? 2 * Staged<D>::kBytes : 16];
+DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& parts, char* staged) {
+  constexpr int RG = 4 / KW, M = 16 * RT * (Call::kHeads ? 1 : RG);
+  constexpr bool DIRECT = KW == 4 || Call::kHeads;
+  static_assert(KW == 1 || (KW == 4 && !Call::kHeads), "the four waves have rows of their own, or heads, or blocks");
+  f32x4* joined = reinterpret_cast<f32x4*>(staged);        // KW == 4: [wave][RT][D / 16][lane]
+  float *joined_m = reinterpret_cast<float*>(joined + 4 * RT * (D / 16) * 64), *joined_l = joined_m + 4 * RT * 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int kw = wave % KW, rg = wave / KW;
   const AttendArgs& p = call.p;
-  const int nb = p.cache.capacity / kBlock, tiles = q.tiles, w = work.w, end = work.end;
+  const int nb = p.cache.capacity / kBlock, tiles = q.tiles, w = work.w, end = work.end, heads = Call::kHeads ? (p.H_kv + 3) / 4 : p.H_kv;
   const float scale_log2 = p.scale * kLog2e;
   Segment& seg = work.seg;
   int pos = work.pos;
@@ -407,9 +414,10 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
   while (true) {
     const int to = min(end, seg.end());
     if (SPLIT && parts.by_segment && tid == 0 && pos == seg.begin)
-      parts.notes[segment_number(seg, p.H_kv, tiles)] = note_of_segment(work.all, w, seg, p.H_kv, tiles);
-    const int b = seg.b, h = seg.h, first_row = seg.t * M + rg * RT * 16;
-    const int blk0 = seg.block_at(pos), blk_end = seg.block_at(to);
+      parts.notes[segment_number(seg, heads, tiles)] = note_of_segment(work.all, w, seg, heads, tiles);
+    const bool idle = Call::kHeads && 4 * seg.h + wave >= p.H_kv;          // there is no such head
+    const int b = seg.b, h = Call::kHeads ? min(4 * seg.h + wave, p.H_kv - 1) : seg.h, first_row = seg.t * M + (Call::kHeads ? 0 : rg * RT * 16);
+    const int blk0 = seg.block_at(pos), blk_end = idle ? blk0 : seg.block_at(to);
     const size_t bh = (size_t)b * p.H_kv + h;
     const unsigned char* K = p.cache.K + bh * p.cache.capacity * D;
     const unsigned char* V = p.cache.V + bh * p.cache.capacity * D;
@@ -436,7 +444,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
       next_v = scale_of(Vs, before.V_scale, blk);
       k.load(codes(K, before.K, blk), at, at_odd);
     };
-    if constexpr (KW == 4) load_key(blk0 + kw);
+    if constexpr (DIRECT) load_key(blk0 + kw);
     int least = 0x7fffffff, limit[RT];
     bf16x8 qf[RT][D / 32];
 #pragma unroll
@@ -466,7 +474,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
         block_step<D, RT>(a, qf, k, v, k_scale, v_scale, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g, after_scores);
       }
     };
-    if constexpr (KW == 1) {
+    if constexpr (!DIRECT) {
       // a wave fetches every fourth piece; PIECES is a multiple of 4
       constexpr int MINE = Staged<D>::PIECES / 4;
       const unsigned buffers = uniform(lds_address(staged));
@@ -481,7 +489,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
         }
       };
       const int in_piece = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), in_odd = r * 32 + g * 8;
-      const bool rows_here = first_row < p.N * p.group;
+      const bool rows_here = first_row < uniform(q.count(b)) * p.group;
       // Scales: 64 blocks' at a time, one in each lane.
       float k_scales = 0.f, v_scales = 0.f;
       auto load_scales = [&](int blk) {
@@ -588,7 +596,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
     if constexpr (!SPLIT) break;
     pos = to;
     if (pos >= end) break;
-    next_segment(q, p.H_kv, seg);
+    next_segment(q, heads, seg);
     seg.blocks = uniform(seg.blocks);
   }
 }

@@ -11,6 +11,7 @@ constexpr int kThreads = kAttendThreads;
 // SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
 template <int D, int RT, int KW, bool SPLIT>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
+  __shared__ __attribute__((aligned(1024))) char staged[kAttendBytes<D, RT, KW>];
   __shared__ Runs runs;
   const Problem q{p.lengths, p.counts, p.cache.capacity, p.N, p.group, p.causal, tiles, 16 * RT * 4 / KW};
   const PlainCall call{p};
@@ -34,7 +35,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_ker
     work.end = work.seg.end();
   }
   work.seg.blocks = uniform(work.seg.blocks);
-  attend<D, RT, KW, SPLIT>(call, q, work, parts);
+  attend<D, RT, KW, SPLIT>(call, q, work, parts, staged);
 }
 
 // Joins the parts of the segments that were split between shares.  blockIdx.x is a note; blockIdx.y one row tile of 16 and DT of the D / 16 column

@@ -64,7 +64,7 @@ def _some(seed, n, lo, hi):
 @pytest.mark.parametrize("d", DIMS)
 @pytest.mark.parametrize("P,S", [(1, 1), (1, 5), (3, 2), (2, 17), (1, 40)])
 def test_single_tokens(lib, d, P, S):
-    for group, Hkv, pcap, cap in ((1, 2, 64, 64), (4, 1, 1088, 128), (3, 2, 320, 192)):
+    for group, Hkv, pcap, cap in ((1, 2, 64, 64), (4, 1, 1088, 128), (3, 2, 320, 192), (1, 3, 192, 64), (2, 9, 128, 128), (4, 4, 640, 192)):
         prefix_lengths = [pcap, 1, 65][:P] if P > 1 else [pcap - 1]
         lengths = [1, 64, cap, 63][:P * S] + _some(d + S, max(0, P * S - 4), 1, cap)
         q, prefix, cache = _problem(S + group, P, S, group, Hkv, 1, d, pcap, prefix_lengths, cap, lengths)
