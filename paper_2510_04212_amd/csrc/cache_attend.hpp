@@ -121,18 +121,32 @@ struct Runs {
   int waves[kAttendThreads / 64];
   Segment segment;
 };
-// units of all items
-DEVI int scan_units(const Problem& q, int items, int run, Runs& runs) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// A thread's units, summed over the threads in front of it in its wave and with its own.
+DEVI int own_units(const Problem& q, int items, int run) {
+  const int tid = threadIdx.x;
   int x = 0;
   for (int i = tid * run; i < min(items, (tid + 1) * run); ++i) x += q.cost(i / q.tiles, i % q.tiles);
+  return x;
+}
+DEVI int scan_in_wave(int x, Runs& runs) {
+  const int tid = threadIdx.x;
   x = (int)sum_to_lane((unsigned)x);
-  if (lane == 63) runs.waves[wave] = x;
-  __syncthreads();
+  if ((tid & 63) == 63) runs.waves[tid >> 6] = x;
+  return x;
+}
+// behind a barrier; another one, and runs.before is there for all
+DEVI void scan_waves(int x, Runs& runs) {
+  const int tid = threadIdx.x, wave = tid >> 6;
 #pragma unroll
   for (int w = 0; w < kAttendThreads / 64 - 1; ++w) x += w < wave ? runs.waves[w] : 0;
   runs.before[tid + 1] = x;
   if (tid == 0) runs.before[0] = 0;
+}
+// units of all items
+DEVI int scan_units(const Problem& q, int items, int run, Runs& runs) {
+  const int x = scan_in_wave(own_units(q, items, run), runs);
+  __syncthreads();
+  scan_waves(x, runs);
   __syncthreads();
   return uniform(runs.before[kAttendThreads]);
 }
@@ -161,6 +175,7 @@ DEVI Segment find_segment(const Problem& q, int B, int H_kv, int run, int pos, R
   s.h = uniform(s.h);
   s.t = uniform(s.t);
   s.begin = uniform(s.begin);
+  s.start = q.start;
   return s;
 }
 
@@ -369,7 +384,7 @@ struct Parts {
 
 // What the segments are over: a call's queries and its cache.
 struct PlainCall {
-  static constexpr bool kJoint = false, kHeads = false;
+  static constexpr bool kJoint = false, kHeads = false, kRealRows = false;
   const AttendArgs& p;
   // a row of the list
   DEVI const unsigned short* query(int b, int head, int query) const { return p.Q.at + b * p.Q.sb + head * p.Q.sh + query * p.Q.sn; }
@@ -394,6 +409,7 @@ constexpr int kAttendBytes = KW == 4 ? 4 * RT * (D / 16) * 64 * 16 + 2 * 4 * RT 
 // Call::kJoint: a segment's blocks are those of its sequence's prefix, then its own.
 // Call::kHeads (KW = 1, few rows): a segment is the same rows of four key/value heads, one for each wave, which reads that head's blocks straight into
 // registers: short segments are begun and ended four at a time, and nothing is joined in LDS.
+// Call::kRealRows: parts hold the real queries' rows alone (few of 16 or 64 rows may be real, and short segments have many parts).
 // staged: kAttendBytes of LDS, 1 KB aligned.
 template <int D, int RT, int KW, bool SPLIT, class Call>
 DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& parts, char* staged) {
@@ -460,6 +476,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
     for (int i = 1; i < 16; i <<= 1) least = min(least, __shfl_xor(least, i));
     least = uniform(least);
 
+    const int real_rows = uniform(q.count(b)) * p.group;
     Acc<D, RT> a;
     a.clear();
     auto step = [&](const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, int blk, auto&& after_scores) {
@@ -489,7 +506,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
         }
       };
       const int in_piece = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), in_odd = r * 32 + g * 8;
-      const bool rows_here = first_row < uniform(q.count(b)) * p.group;
+      const bool rows_here = first_row < real_rows;
       // Scales: 64 blocks' at a time, one in each lane.
       float k_scales = 0.f, v_scales = 0.f;
       auto load_scales = [&](int blk) {
@@ -542,6 +559,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
         call.template store<DT, M>(seg, tile, o, m, l, dt0, lane);
         return;
       }
+      if (Call::kRealRows && seg.t * M + (Call::kHeads ? 0 : tile * 16) + r >= real_rows) return;
 #pragma unroll
       for (int i = 0; i < DT; ++i) reinterpret_cast<f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + lane] = o[i];
       float* ml = slot + RG * RT * (D / 16 * 256) + tile * 32;

@@ -1,11 +1,12 @@
 // Attention of sequences that continue prefixes they share with others (attn_cache_fwd_shared of include/attn.h).
 #include "cache_attend.hpp"
+#include <algorithm>
 
 namespace {
 
 // Every segment reads its sequence's prefix, then its own blocks.
 struct JointCall {
-  static constexpr bool kJoint = true, kHeads = false;
+  static constexpr bool kJoint = true, kHeads = false, kRealRows = false;
   const AttendArgs& p;
   const SharedArgs& all;
   DEVI int length(int b) const { return uniform(min(max(all.prefix_lengths[b / all.S], 0), all.prefix.capacity)); }
@@ -43,7 +44,9 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attn_cache_j
 }
 
 // ---- shared: two lists of segments in one launch, the prefixes' (rows: the real queries of a prefix's sequences, one after the other) and the sequences'
-// own.  The work-groups are dealt to the lists by what their units cost, and every segment leaves its rows' sums, whole or in parts, for the joining kernel.
+// own.  Every segment leaves its rows' sums, whole or in parts, for the joining kernel.  The prefixes' are shared out to work-groups as in
+// attn_cache_fwd, to as many of those that run at once as what their units cost against the own ones' says; own ones have a work-group each, or, where they are
+// long, are shared out to the rest.
 struct List {
   Join* notes;                             // one for each segment
   float* slots;                            // parts of segments: two for each work-group
@@ -55,15 +58,20 @@ struct List {
 struct SharedPlan {
   AttendArgs prefix;                       // the prefixes as sequences: P of them, of up to S * N queries each
   const int* starts;                       // [P * S]: real queries of its prefix's sequences in front of this one; NULL: all are real
-  int groups;                              // work-groups: a multiple of 8, 16 at least
+  int groups;                              // work-groups that the lists are shared out to: a multiple of 8, 16 at least
+  bool own_split;                          // the own list is; otherwise a work-group for each of its segments follows
   List prefixes, own;
 };
+
+// What four heads' segments cost to begin and end, in blocks of theirs.
+constexpr int kHeadsStart = 1;
+template <int KW, bool HEADS> constexpr int kLeast = HEADS ? kHeadsStart + 1 : kLeastUnits<KW>;
 
 // 16-row tiles of a slot: sums of their rows, then maxima and sums of probabilities
 template <int D> constexpr int kTileFloats = D / 16 * 256 + 32;
 
 template <int D, int TILES, bool PREFIX, bool HEADS> struct ListCall {
-  static constexpr bool kJoint = false, kHeads = HEADS;
+  static constexpr bool kJoint = false, kHeads = HEADS, kRealRows = true;
   const AttendArgs& p;
   const SharedPlan& plan;
   int N, S;                                // (of the prefixes)
@@ -132,37 +140,51 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attn_cache_s
   __shared__ Runs runs, own_runs;
   const AttendArgs &p = plan.prefix, &o = a.own;
   const Problem q{p.lengths, p.counts, p.cache.capacity, p.N, p.group, 0, plan.prefixes.tiles, 16 * RT * 4 / KW};
-  const Problem own{o.lengths, o.counts, o.cache.capacity, o.N, o.group, o.causal, plan.own.tiles, HEADS ? 16 : 16 * ORT * 4 / OKW};
+  const Problem own{o.lengths, o.counts, o.cache.capacity, o.N, o.group, o.causal, plan.own.tiles, HEADS ? 16 : 16 * ORT * 4 / OKW, HEADS ? kHeadsStart : kStart};
   const int run = (p.B * q.tiles + kAttendThreads - 1) / kAttendThreads, own_run = (o.B * own.tiles + kAttendThreads - 1) / kAttendThreads;
-  const int units = plan.prefixes.heads * scan_units(q, p.B * q.tiles, run, runs), own_units = plan.own.heads * scan_units(own, o.B * own.tiles, own_run, own_runs);
-  const int eighths = plan.groups / 8;
-  const long long cost = (long long)units * plan.prefixes.cost, own_cost = (long long)own_units * plan.own.cost;
-  const int groups = 8 * uniform(min(max((int)((eighths * cost + (cost + own_cost) / 2) / (cost + own_cost)), 1), eighths - 1));
-  auto begin = [&](const Problem& problem, const List& list, int B, int total, int most, int least, int runs_of, Runs& runs, int group, Work& work) {
-    work.all = shares_of(total, most, least);
-    work.w = share_of(group, work.all.number);
-    if (work.w < 0) return false;
+  Work work;
+  if ((int)blockIdx.x >= plan.groups) {    // an own segment
+    const int i = blockIdx.x - plan.groups;
+    work.seg = Segment{i / own.tiles / plan.own.heads, i / own.tiles % plan.own.heads, i % own.tiles, 0, 0, own.start};
+    work.seg.blocks = uniform(own.blocks(work.seg.b, work.seg.t));
+    work.pos = 0;
+    work.end = work.seg.end();
+    work.w = 0;
+    work.all = Shares{1, work.end, 0};
+  } else {
+    int x = own_units(q, p.B * q.tiles, run), own_x = own_units(own, o.B * own.tiles, own_run);          // (both lists' loads at once)
+    x = scan_in_wave(x, runs);
+    own_x = scan_in_wave(own_x, own_runs);
+    __syncthreads();
+    scan_waves(x, runs);
+    scan_waves(own_x, own_runs);
+    __syncthreads();
+    const int units = plan.prefixes.heads * uniform(runs.before[kAttendThreads]), own_all = plan.own.heads * uniform(own_runs.before[kAttendThreads]);
+    const int eighths = plan.groups / 8;
+    const long long cost = (long long)units * plan.prefixes.cost, own_cost = (long long)own_all * plan.own.cost;
+    const int groups = 8 * uniform(min(max((int)((eighths * cost + (cost + own_cost) / 2) / (cost + own_cost)), 1), eighths - 1));
+    const bool of_prefix = (int)blockIdx.x < groups;
+    if (!of_prefix && !plan.own_split) return;
+    work.all = of_prefix ? shares_of(units, groups, kLeastUnits<KW>) : shares_of(own_all, plan.groups - groups, kLeast<OKW, HEADS>);
+    work.w = share_of(of_prefix ? blockIdx.x : blockIdx.x - groups, work.all.number);
+    if (work.w < 0) return;
     work.pos = uniform(work.all.begin(work.w));
     work.end = uniform(work.all.begin(work.w + 1));
-    work.seg = find_segment(problem, B, list.heads, runs_of, work.pos, runs);
+    work.seg = of_prefix ? find_segment(q, p.B, plan.prefixes.heads, run, work.pos, runs) : find_segment(own, o.B, plan.own.heads, own_run, work.pos, own_runs);
     work.seg.blocks = uniform(work.seg.blocks);
-    return true;
-  };
-  Work work;
-  if ((int)blockIdx.x < groups) {
-    if (!begin(q, plan.prefixes, p.B, units, groups, kLeastUnits<KW>, run, runs, blockIdx.x, work)) return;
-    attend<D, RT, KW, true>(ListCall<D, RT * 4 / KW, true, false>{p, plan, o.N, a.S}, q, work, Parts{plan.prefixes.notes, plan.prefixes.slots, true}, staged);
-  } else {
-    if (!begin(own, plan.own, o.B, own_units, plan.groups - groups, kLeastUnits<OKW>, own_run, own_runs, blockIdx.x - groups, work)) return;
-    attend<D, ORT, OKW, true>(ListCall<D, ORT * 4 / OKW, false, HEADS>{o, plan, 0, 0}, own, work, Parts{plan.own.notes, plan.own.slots, true}, staged);
+    if (of_prefix) {
+      attend<D, RT, KW, true>(ListCall<D, RT * 4 / KW, true, false>{p, plan, o.N, a.S}, q, work, Parts{plan.prefixes.notes, plan.prefixes.slots, true}, staged);
+      return;
+    }
   }
+  attend<D, ORT, OKW, true>(ListCall<D, ORT * 4 / OKW, false, HEADS>{o, plan, 0, 0}, own, work, Parts{plan.own.notes, plan.own.slots, true}, staged);
 }
 
 // Joins a row's parts: those of its prefix's segment and those of its own.  blockIdx: 16 rows of a prefix's sequences, padding included; the head, and DT of
 // the D / 16 column tiles; the prefix.  NW waves take every NW-th part and join theirs in LDS.
 template <int D, int RT, int KW, int ORT, int OKW, bool HEADS, int NW, int DT>
 __global__ __launch_bounds__(64 * NW) void attn_cache_shared_merge_kernel(SharedArgs a, SharedPlan plan) {
-  constexpr int TILES = RT * 4 / KW, OTILES = ORT * 4 / OKW, PARTS = D / 16 / DT;
+  constexpr int TILES = RT * 4 / KW, OTILES = ORT * 4 / OKW, PARTS = D / 16 / DT, kAhead = DT <= 2 ? 4 : DT <= 8 ? 2 : 1;
   __shared__ f32x4 joined[NW][DT][64];
   __shared__ float joined_ml[2][NW][16];
   const AttendArgs& p = a.own;
@@ -174,41 +196,63 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_shared_merge_kernel(Shared
   const bool real = there && own_row < real_count(p.counts, b, p.N) * p.group;
   const int in_prefix = plan.starts ? plan.starts[b] * p.group + own_row : row;             // its row of the prefix's list
 
+  // where the row's parts lie: in its prefix's segment, then in its own
+  constexpr int OM = HEADS ? 16 : 16 * OTILES;
+  const int t = in_prefix / (16 * TILES), at = in_prefix % (16 * TILES), own_tile = HEADS ? h % 4 : own_row % OM / 16;
+  const int segment = plan.prefixes.segment(item, h, t), own_segment = plan.own.segment(b, HEADS ? h / 4 : h, own_row / OM);
+  Join j{0, 0, 0, 0}, k{0, 0, 0, 0};
+  if (real) {
+    j = plan.prefixes.notes[segment];
+    k = plan.own.notes[own_segment];
+  }
+  const int parts = real ? max(j.parts, 1) : 0, all = real ? parts + max(k.parts, 1) : 0;
+  auto slot_of = [&](int part) {
+    if (part < parts)
+      return j.parts == 0 ? plan.prefixes.whole + (size_t)segment * (TILES * kTileFloats<D>)
+                          : plan.prefixes.slots + (size_t)joined_slot(j.first, part) * (TILES * kTileFloats<D>);
+    return k.parts == 0 ? plan.own.whole + (size_t)own_segment * (OTILES * kTileFloats<D>)
+                        : plan.own.slots + (size_t)joined_slot(k.first, part - parts) * (OTILES * kTileFloats<D>);
+  };
   f32x4 o[DT];
   float m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
-  // the parts of row `at` of a list's segment, in its 16-row tile `tile`
-  auto add = [&](const List& list, int tiles, int segment, int tile, int at, int first) {
-    Join j{0, 0, 0, 0};
-    if (real) j = list.notes[segment];
-    const int parts = !real ? 0 : j.parts == 0 ? 1 : j.parts;
-    for (int part = first; __any(part < parts); part += NW) {
-      const float* slot = j.parts == 0 ? list.whole + (size_t)segment * (tiles * kTileFloats<D>)
-                                       : list.slots + (size_t)joined_slot(j.first, part) * (tiles * kTileFloats<D>);
-      f32x4 x[DT];
-      float mp = -INFINITY, lp = 0.f;
+  for (int part = wave; __any(part < all); part += NW * kAhead) {
+    f32x4 x[kAhead][DT];
+    float mp[kAhead], lp[kAhead];
 #pragma unroll
-      for (int i = 0; i < DT; ++i) x[i] = f32x4{0, 0, 0, 0};
-      if (part < parts) {
+    for (int a = 0; a < kAhead; ++a) {
+      mp[a] = -INFINITY;
+      lp[a] = 0.f;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) x[i] = reinterpret_cast<const f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + 16 * g + at];
-        const float* ml = slot + tiles * (D / 16 * 256) + tile * 32;
-        mp = ml[at];
-        lp = ml[16 + at];
-      }
-      const float most = fmaxf(m, mp), use = most == -INFINITY ? 0.f : most;
-      const float mine = __builtin_amdgcn_exp2f(m - use), theirs = __builtin_amdgcn_exp2f(mp - use);
-      l = l * mine + lp * theirs;
+      for (int i = 0; i < DT; ++i) x[a][i] = f32x4{0, 0, 0, 0};
+      const int this_part = part + a * NW;
+      if (this_part >= all) continue;
+      const bool first = this_part < parts;
+      const float* slot = slot_of(this_part);
+      const int tile = first ? at / 16 : own_tile, in_tile = first ? at % 16 : own_row % 16;
 #pragma unroll
-      for (int i = 0; i < DT; ++i) o[i] = o[i] * mine + x[i] * theirs;
-      m = most;
+      for (int i = 0; i < DT; ++i) x[a][i] = reinterpret_cast<const f32x4*>(slot)[(tile * (D / 16) + dt0 + i) * 64 + 16 * g + in_tile];
+      const float* ml = slot + (first ? TILES : OTILES) * (D / 16 * 256) + tile * 32;
+      mp[a] = ml[in_tile];
+      lp[a] = ml[16 + in_tile];
     }
-  };
-  const int t = in_prefix / (16 * TILES), at = in_prefix % (16 * TILES);
-  add(plan.prefixes, TILES, plan.prefixes.segment(item, h, t), at / 16, at % 16, wave);
-  constexpr int OM = HEADS ? 16 : 16 * OTILES;             // (the waves without a prefix's part first)
-  add(plan.own, OTILES, plan.own.segment(b, HEADS ? h / 4 : h, own_row / OM), HEADS ? h % 4 : own_row % OM / 16, own_row % 16, NW - 1 - wave);
+    float most = m;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) most = fmaxf(most, mp[a]);
+    const float use = most == -INFINITY ? 0.f : most, mine = __builtin_amdgcn_exp2f(m - use);
+    l *= mine;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] *= mine;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const float theirs = __builtin_amdgcn_exp2f(mp[a] - use);
+      l += lp[a] * theirs;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] += x[a][i] * theirs;
+    }
+    m = most;
+  }
 
   if (g == 0) { joined_ml[0][wave][r] = m; joined_ml[1][wave][r] = l; }
 #pragma unroll
@@ -237,7 +281,7 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_shared_merge_kernel(Shared
 // Which form serves a call, and what it needs.
 struct SharedForm {
   CacheForm prefix, own;
-  bool shared, heads;                      // heads: four key/value heads of a sequence's own make a segment
+  bool shared, own_split, heads;           // heads: four key/value heads of a sequence's own make a segment
   int own_heads, groups;
   long long segments, own_segments;
   // notes, parts, whole segments, starts and totals of real queries
@@ -249,19 +293,41 @@ struct SharedForm {
   }
   size_t slot_floats_own(int d) const { return heads ? 4 * (size_t)(d / 16 * 256 + 32) : own.slot_floats(d); }
 };
+// Estimates in us, from capacities.  Joint: one launch, bound by a segment's chain of blocks, by all segments' reads through the caches (10.5 TB/s), by
+// what has to come from memory (5.2), or by the vector and matrix units.  Shared: finding the work, parts and a second launch cost 12 us and more, and then a prefix
+// is read once.  us, joint / shared, P x S, H 32/8, d 128, own 16 to 128 tokens of 128: prefixes of 1024: 1x4 10.3 / 13.8, 1x16 10.3 / 17.1, 8x4 11.5 / 16.7,
+// 1x64 17.6 / 21.3, 4x32 32.1 / 25.7, 16x8 32.2 / 25.3;  of 2048: 1x4 15.7 / 14.8, 8x4 16.7 / 19.7, 1x64 28.1 / 22.5, 16x8 55.6 / 33.5;  of 512: 16x8 22.0 / 22.7;  S = 1:
+// 64x1 of 1024 29.2 / 43.5;  16 queries, 1x8 of 1024: 23.7 / 25.3;  64 queries, 2x4 of 2048: 58.5 / 49.9;  d 64, H 12/12: 1x4 of 2048 10.2 / 12.7, 16x8 of 1024 22.2 / 17.9.
+bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double P, double S, double H_kv, int d, int prefix_blocks, int blocks) {
+  const double wide = d / 128.0, megabytes = 128e-6 * d, segments = P * S * H_kv * own.tiles, all = prefix_blocks + blocks;
+  auto busy = [&](const CacheForm& f, double number) { return number * wide * (f.KW == 4 ? 0.7 : f.RT == 1 ? 1.3 : 2.0) / 512; };
+  const double chain = all * wide * (own.KW == 4 ? 0.33 : own.RT == 1 ? 1.05 : 1.6);
+  const double once = P * H_kv * ((double)prefix_blocks + S * blocks) * megabytes;
+  const double joint = 4.5 + std::max(std::max(chain, segments * all * megabytes / 10.5), std::max(once / 5.2, own.KW == 4 ? 0.0 : busy(own, segments * all)));
+  const double shared = 12 + (own.KW == 4 ? 0 : 8) + wide * (1.5 + 0.006 * P * S * H_kv) +
+                        std::max(once / 6, busy(prefix, P * H_kv * prefix.tiles * prefix_blocks) + busy(own, segments * blocks));
+  return joint < shared;
+}
+// Own segments of up to 16 rows have a work-group each where attn_cache_fwd's rule says so; up to four blocks, four heads have one (us, four heads / one: 16 x 8 of
+// 1024, own 128: 25.3 / 29.5; of 4096, own 512: 58 / 55.5).  More rows are shared out (64 queries each of 2 x 8, prefixes of 8192, own 1024: 108 us, and 124 whole).
+// Prefixes of more than 64 rows: two row tiles a wave where a share has ten blocks or so (256 rows of 8192: 39.8 us, and 31.9 with one; 128 of 131072: 61 and 66).
 SharedForm shared_form(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity) {
   SharedForm f;
   const long long rows = (long long)N * (H / H_kv);
+  const int room = d == 256 ? 256 : 512;   // as many work-groups run at once
   f.prefix = row_form(rows * S);
-  f.own = row_form(rows);
-  f.heads = f.own.KW == 4 && H_kv >= 3;
+  f.own = cache_form(P * S, H, H_kv, N, d, capacity);
+  if (f.prefix.RT == 2 && f.own.RT == 1 && cache_units(P, H_kv, f.prefix, prefix_capacity) < 10.0 * room) f.prefix.set_rows(rows * S, 1);
+  f.heads = f.own.KW == 4 && H_kv >= 3 && (f.own.split || capacity <= 4 * kBlock);
   f.own_heads = f.heads ? (H_kv + 3) / 4 : H_kv;
   f.segments = (long long)P * H_kv * f.prefix.tiles;
   f.own_segments = (long long)P * S * f.own_heads * f.own.tiles;
-  f.shared = true;
-  auto shares = [](const CacheForm& form, bool heads, double units) { return units / (form.KW == 4 && !heads ? kLeastUnits<4> : kLeastUnits<1>); };
-  const double most = shares(f.prefix, false, cache_units(P, H_kv, f.prefix, prefix_capacity)) + shares(f.own, f.heads, cache_units(P * S, f.own_heads, f.own, capacity)) + 16;
-  const int room = d == 256 ? 256 : 512;   // as many as run at once
+  f.own_split = f.own.split || f.own.KW == 1 || f.own_segments > 1 << 20;
+  f.shared = f.own.tiles > 65535 || !joint_is_faster(f.prefix, f.own, P, S, H_kv, d, prefix_capacity / kBlock, capacity / kBlock);
+  auto shares = [&](const CacheForm& form, bool heads, int B, int H_kv, int capacity) {
+    return cache_units(B, H_kv, form, capacity, heads ? kHeadsStart : kStart) / (heads ? kLeast<1, true> : form.KW == 4 ? kLeast<4, false> : kLeast<1, false>);
+  };
+  const double most = shares(f.prefix, false, P, H_kv, prefix_capacity) + shares(f.own, f.heads, P * S, f.own_heads, capacity) + 16;
   f.groups = most >= room ? room : (int)most / 8 * 8;
   return f;
 }
@@ -292,6 +358,7 @@ template <int D, int RT, int KW, int ORT, int OKW, bool HEADS> hipError_t launch
   plan.prefix.causal = 0;
   plan.starts = p.counts ? integers : nullptr;
   plan.groups = f.groups;
+  plan.own_split = f.own_split;
   plan.prefixes.heads = p.H_kv;
   plan.prefixes.tiles = f.prefix.tiles;
   plan.prefixes.cost = unit_cost(f.prefix, false);
@@ -304,7 +371,7 @@ template <int D, int RT, int KW, int ORT, int OKW, bool HEADS> hipError_t launch
     attn_cache_starts_kernel<<<(unsigned)a.P, kAttendThreads, 0, stream>>>(p.counts, a.S, p.N, integers, integers + (size_t)a.P * a.S);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  attn_cache_shared_kernel<D, RT, KW, ORT, OKW, HEADS><<<(unsigned)f.groups, kAttendThreads, 0, stream>>>(a, plan);
+  attn_cache_shared_kernel<D, RT, KW, ORT, OKW, HEADS><<<(unsigned)(f.groups + (f.own_split ? 0 : f.own_segments)), kAttendThreads, 0, stream>>>(a, plan);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (f.groups > 4 * f.segments)
     attn_cache_shared_merge_kernel<D, RT, KW, ORT, OKW, HEADS, 16, 2><<<dim3(row_tiles, (unsigned)(p.H_kv * (D / 32)), (unsigned)a.P), 1024, 0, stream>>>(a, plan);
@@ -335,7 +402,6 @@ template <int D> hipError_t launch(const SharedArgs& a, hipStream_t stream) {
     if (f.own.RT == 1) return f.prefix.RT == 1 ? launch_shared<D, 1, 1, 1, 1, false>(a, f, stream) : launch_shared<D, 2, 1, 1, 1, false>(a, f, stream);
     return launch_shared<D, 2, 1, 2, 1, false>(a, f, stream);
   }
-  if (f.own.tiles > 65535) return hipErrorInvalidConfiguration;
   if (f.own.KW == 4) return launch_joint<D, 1, 4>(a, f.own, stream);
   if (f.own.RT == 1) return launch_joint<D, 1, 1>(a, f.own, stream);
   return launch_joint<D, 2, 1>(a, f.own, stream);

@@ -25,6 +25,7 @@ constexpr int kBlock = 64;                 // tokens that share a scale; the hea
 struct Problem {
   const int *lengths, *counts;             // counts may be NULL
   int capacity, N, group, causal, tiles, M;     // M rows (query * group + head of the group) per tile
+  int start = kStart;                      // what a segment costs beside its blocks
   // of the N queries, those that sequence b really has
   SHARES_FN int count(int b) const {
     if (!counts) return N;
@@ -41,7 +42,7 @@ struct Problem {
     if (seen > all) seen = all;
     return seen > 0 ? (int)((seen + kBlock - 1) / kBlock) : 0;
   }
-  SHARES_FN int cost(int b, int t) const { return kStart + blocks(b, t); }
+  SHARES_FN int cost(int b, int t) const { return start + blocks(b, t); }
 };
 
 // Units of a call, counted in int: below this (where the entry point refuses the call), so that sums of two stay in range.
@@ -51,9 +52,10 @@ struct Segment {
   int b, h, t;
   int begin;                               // of its units in the whole list
   int blocks;
-  SHARES_FN int end() const { return begin + kStart + blocks; }
+  int start;                               // the list's
+  SHARES_FN int end() const { return begin + start + blocks; }
   SHARES_FN int block_at(int pos) const {  // the first block at or behind a unit of it
-    const int i = pos - begin - kStart;
+    const int i = pos - begin - start;
     return i > 0 ? i : 0;
   }
 };
@@ -66,8 +68,8 @@ SHARES_FN bool locate(const Problem& q, int b, int t, int first, int each, int a
   const int h = rest / each;
   rest -= h * each;
   const int blocks = q.blocks(b, t);
-  if (rest < at || rest >= at + kStart + blocks) return false;
-  *s = Segment{b, h, t, pos - (rest - at), blocks};
+  if (rest < at || rest >= at + q.start + blocks) return false;
+  *s = Segment{b, h, t, pos - (rest - at), blocks, q.start};
   return true;
 }
 // The one behind it; there is one.
@@ -131,6 +133,10 @@ struct CacheForm {
   int RT, KW, tiles, shares;
   bool split;                              // shared out; otherwise a work-group per segment and nothing to join
   int rows() const { return 16 * RT * 4 / KW; }
+  void set_rows(long long number, int row_tiles) {
+    RT = row_tiles;
+    tiles = (int)((number + rows() - 1) / rows());
+  }
   size_t slot_floats(int d) const { return (size_t)(4 / KW) * RT * (d / 16 * 256 + 32); }
   bool many_parts;                         // few segments for the shares: each is in many parts
   // notes, then slots
@@ -139,8 +145,8 @@ struct CacheForm {
 // No share is smaller.  Four waves that share the blocks out: one block; sharing them: two (20 rows of 4 sequences of 1000 tokens, H 32/8, d 128: 24.7 us
 // at eight blocks, 21.5 at four, 19.7 at two; 64 rows of 32768: 33.3, 28.7, 29.6; 8400 rows of 2100: 70.8, 73.6, 73.9).
 template <int KW> constexpr int kLeastUnits = kStart + (KW == 4 ? 1 : 2);
-inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
-  return (double)B * H_kv * f.tiles * (kStart + capacity / kBlock);
+inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity, int start = kStart) {
+  return (double)B * H_kv * f.tiles * (start + capacity / kBlock);
 }
 // Figures come in pairs, both sides measured on the code of that step; later steps made both faster.
 // Rows.  Up to 16: each wave takes blocks of its own (one token of 64 sequences of 4300, H 32/8, d 128: 102 us, and 116 with the blocks
@@ -158,9 +164,8 @@ inline double cache_units(int B, int H_kv, const CacheForm& f, int capacity) {
 //     4096: 4 61 / 28.  2048 queries of 2048 tokens 65 / 71, 4096 of 4096 197 / 175.
 inline CacheForm row_form(long long rows) {
   CacheForm f{};
-  f.RT = rows <= 64 ? 1 : 2;
   f.KW = rows <= 16 ? 4 : 1;
-  f.tiles = (int)((rows + f.rows() - 1) / f.rows());
+  f.set_rows(rows, rows <= 64 ? 1 : 2);
   return f;
 }
 inline CacheForm cache_form(int B, int H, int H_kv, int N, int d, int capacity) {
