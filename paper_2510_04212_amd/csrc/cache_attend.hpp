@@ -476,7 +476,7 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
     for (int i = 1; i < 16; i <<= 1) least = min(least, __shfl_xor(least, i));
     least = uniform(least);
 
-    const int real_rows = uniform(q.count(b)) * p.group;
+    const int real_rows = (Call::kRealRows ? uniform(q.count(b)) : p.N) * p.group;
     Acc<D, RT> a;
     a.clear();
     auto step = [&](const KCodes<D>& k, VCodes<D>& v, float k_scale, float v_scale, int blk, auto&& after_scores) {
@@ -502,7 +502,8 @@ DEVI void attend(const Call& call, const Problem& q, Work& work, const Parts& pa
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
           const int piece = wave + 4 * i;
-          fetch_piece(piece < Staged<D>::KP ? codes(K, before.K, blk) : codes(V, before.V, blk), from[i], buffers + buffer * Staged<D>::kBytes + piece * 1024);
+          const bool key = piece < Staged<D>::KP;
+          fetch_piece(codes(key ? K : V, key ? before.K : before.V, blk), from[i], buffers + buffer * Staged<D>::kBytes + piece * 1024);
         }
       };
       const int in_piece = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), in_odd = r * 32 + g * 8;

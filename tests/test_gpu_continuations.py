@@ -83,6 +83,90 @@ def test_chunks(lib, d, causal):
         _run(q, prefix, prefix_lengths, cache, lengths, None, d ** -0.5, causal, f"N {N}")
 
 
+def _values_on_gpu(c):
+    """K and V of a cache in 64 bits, [B,Hkv,cap,d]."""
+    B, Hkv, cap, d = c.K.shape
+    k = c.K.double().view(B, Hkv, -1, 64, d) * c.K_scale.double()[..., None, None]
+    v = (c.V.double() * c.V_scale.double()[..., None, None]).transpose(3, 4)
+    return k.reshape(B, Hkv, cap, d), v.reshape(B, Hkv, cap, d)
+
+
+def _check_on_gpu(q, prefix, prefix_lengths, cache, lengths, counts, alpha, causal, O, lse, label=""):
+    """As _check, for sizes that numpy is slow for: the same definition in 64 bits in torch, a sequence and key/value head at a time."""
+    B, H, N, d = q.shape
+    (Kp, Vp), (K, V) = _values_on_gpu(prefix), _values_on_gpu(cache)
+    S, Hkv = B // Kp.shape[0], K.shape[1]
+    group = H // Hkv
+    for b in range(B) if B <= 24 else sorted({0, 1, S - 1, B - S, B - 2, B - 1, *range(0, B, 7)}):
+        n, length, before = counts[b], lengths[b], prefix_lengths[b // S]
+        assert (O[b, :, n:] == 0).all() and torch.isneginf(lse[b, :, n:]).all(), (label, b)
+        for h in range(Hkv if n and before + length else 0):
+            k, v = torch.cat((Kp[b // S, h, :before], K[b, h, :length])), torch.cat((Vp[b // S, h, :before], V[b, h, :length]))
+            x = q[b, h * group:(h + 1) * group, :n].double().reshape(-1, d)
+            s = alpha * (x @ k.t())
+            own = length - n + 1 + torch.arange(n, device=DEV) if causal else torch.full((n,), length, device=DEV)
+            hidden = torch.arange(before + length, device=DEV) >= before + own.clamp(0, length)[:, None]
+            s = s.view(group, n, -1).masked_fill(hidden, -float("inf")).view(group * n, -1)
+            l, p = torch.logsumexp(s, 1), torch.softmax(s, 1)
+            e = 2 * (d + 4) * 2.0 ** -24 * alpha * (x.abs() @ k.abs().t()).amax(1) + 2.0 ** -22 * (alpha * (x @ k.t())).abs().amax(1) + 2.0 ** -16
+            rows = slice(h * group, (h + 1) * group)
+            off = ((lse[b, rows, :n].double().reshape(-1) - l).abs() - e).max().item()
+            assert off <= 0, (label, "LSE", b, h, off)
+            o = p @ v
+            tol = 2.0 ** -8 * o.abs() + (2.0 ** -8 + e[:, None]) * 1.01 * (p @ v.abs() + o.abs())
+            off = ((O[b, rows, :n].double().reshape(-1, d) - o).abs() - tol).max().item()
+            assert off <= 0, (label, "O", b, h, off)
+
+
+def _fill_on_gpu(seed, B, Hkv, cap, d, lengths):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    c, n = _garbage(B, Hkv, cap, d), max(lengths)
+    k, v = (torch.randn((B, Hkv, n, d), generator=g, device=DEV) * torch.exp2(torch.randint(-2, 3, (B, Hkv, n, 1), generator=g, device=DEV).float()) for _ in range(2))
+    binding.attn_cache_append(c, (0.5 * k).bfloat16(), v.bfloat16(), _i32(lengths), _i32(lengths))
+    return c
+
+
+@pytest.mark.parametrize("d", DIMS)
+@pytest.mark.parametrize("P,S,Hkv,group,N,pcap,cap", [
+    (1, 3, 2, 2, 1, 8192, 128),             # up to 16 rows a prefix; own heads one to a work-group
+    (2, 2, 5, 3, 1, 8192, 192),             # own heads four to a work-group, the last one alone
+    (1, 40, 4, 1, 1, 9600, 64),             # up to 64 rows
+    (1, 40, 3, 1, 1, 9600, 448),            # with own segments of a work-group each
+    (2, 3, 3, 2, 2, 4096, 3200),            # and with long ones, shared out
+    (1, 30, 2, 5, 1, 9600, 64),             # several tiles of 64
+    (2, 64, 8, 4, 1, 10240, 128),           # of 128, own heads four to a work-group
+    (2, 64, 8, 4, 1, 10240, 320),           # or one
+    (1, 5, 2, 4, 7, 4096, 128),             # 28 rows of a sequence
+    (1, 12, 8, 3, 16, 8192, 64),            # 48, and tiles of 128 of the prefix
+    (2, 3, 1, 3, 45, 3200, 640),            # 135
+])
+def test_prefixes_that_are_read_once(lib, d, P, S, Hkv, group, N, pcap, cap):
+    """Every pair of forms of the two lists, with padded batches and without."""
+    assert binding.cache_fwd_shared_workspace_bytes(P, S, group * Hkv, Hkv, N, d, pcap, cap) > 0
+    prefix_lengths = [pcap - 5, pcap // 2 + 64][:P]
+    lengths = [cap, N] + [min(cap, N + x) for x in _some(N + S, P * S - 2, 0, cap)]
+    counts = [0, N] + _some(d + S, P * S - 2, 0, N)
+    prefix, cache = _fill_on_gpu(S, P, Hkv, pcap, d, prefix_lengths), _fill_on_gpu(N, P * S, Hkv, cap, d, lengths)
+    g = torch.Generator(device=DEV).manual_seed(d)
+    q = torch.randn((P * S, group * Hkv, N, d), generator=g, device=DEV).bfloat16()
+    for c, causal in ((None, True), (counts, True), (counts, False)):
+        O, lse = binding.attn_cache_fwd_shared(q, prefix, _i32(prefix_lengths), cache, _i32(lengths), d ** -0.5, causal, None if c is None else _i32(c))
+        _check_on_gpu(q, prefix, prefix_lengths, cache, lengths, [N] * (P * S) if c is None else c, d ** -0.5, causal, O, lse, f"{c is None} {causal}")
+    # ends of lengths: an empty prefix, empty caches, nobody real
+    zero = [0] * (P * S)
+    for pl, l, c in ((([0] * P), lengths, counts), (prefix_lengths, zero, None), ([0] * P, zero, None), (prefix_lengths, lengths, zero)):
+        O, lse = binding.attn_cache_fwd_shared(q, prefix, _i32(pl), cache, _i32(l), d ** -0.5, True, None if c is None else _i32(c))
+        _check_on_gpu(q, prefix, pl, cache, l, [N] * (P * S) if c is None else c, d ** -0.5, True, O, lse, "ends")
+        if not any(pl) and not any(l):
+            assert (O == 0).all() and torch.isneginf(lse).all()
+    # lengths and counts that no cache has: full, empty, all, none
+    wild = [[2 ** 31 - 1, -7, cap, -2 ** 31][i % 4] for i in range(P * S)]
+    full = _fill_on_gpu(3, P * S, Hkv, cap, d, [cap] * (P * S))
+    O, lse = binding.attn_cache_fwd_shared(q, prefix, _i32([-1, 2 ** 31 - 1][:P]), full, _i32(wild), d ** -0.5, False, _i32([[N + 9, 2 ** 31 - 1, -1][i % 3] for i in range(P * S)]))
+    if P == 1:
+        _check_on_gpu(q, prefix, [0], full, [min(max(w, 0), cap) for w in wild], [[N, N, 0][i % 3] for i in range(P * S)], d ** -0.5, False, O, lse, "wild")
+
+
 @pytest.mark.parametrize("N", (1, 7, 30))
 def test_lengths_at_their_ends(lib, N):
     """Empty prefixes, empty caches, queries without tokens of their own, padded sequences, all together; and lengths that no cache has."""
@@ -105,10 +189,9 @@ def test_lengths_at_their_ends(lib, N):
 def test_nan_and_infinities_stay_where_they_are_seen(lib):
     """NaN in what a masked place holds, behind the ends of prefix and cache, and in a later query's token, reaches nobody who does not see it."""
     d, Hkv, N = 64, 1, 4
-    for S, group in ((3, 2), (20, 4)):
-        g = _gen(S)
-        prefix_lengths, lengths = [100], [5 + s for s in range(S)]
-        q, prefix, cache = _problem(S, 1, S, group, Hkv, N, d, 128, prefix_lengths, 64, lengths)
+    for S, group, pcap in ((3, 2, 128), (20, 4, 128), (20, 4, 8192)):
+        prefix_lengths, lengths = [pcap - 28], [5 + s for s in range(S)]
+        q, prefix, cache = _problem(S, 1, S, group, Hkv, N, d, pcap, prefix_lengths, 64, lengths)
         want = binding.attn_cache_fwd_shared(q, prefix, _i32(prefix_lengths), cache, _i32(lengths), 0.125)
         for c, n in ((prefix, prefix_lengths), (cache, lengths)):
             for b, l in enumerate(n):
@@ -129,9 +212,10 @@ def test_nan_and_infinities_stay_where_they_are_seen(lib):
         assert torch.isnan(O[..., 3]).all() and not torch.isnan(O[..., 4]).any()
 
 
-def test_strides_outputs_workspaces_and_streams(lib):
-    P, S, Hkv, group, N, d, pcap, cap = 2, 9, 2, 4, 3, 96, 1600, 192
-    prefix_lengths, lengths = [1600, 700], _some(1, P * S, N, cap)
+@pytest.mark.parametrize("pcap", (1600, 6400))              # read for each sequence; read once
+def test_strides_outputs_workspaces_and_streams(lib, pcap):
+    P, S, Hkv, group, N, d, cap = 2, 9, 2, 4, 3, 96, 192
+    prefix_lengths, lengths = [pcap, 700], _some(1, P * S, N, cap)
     q, prefix, cache = _problem(5, P, S, group, Hkv, N, d, pcap, prefix_lengths, cap, lengths)
     H = group * Hkv
     want = _run(q, prefix, prefix_lengths, cache, lengths)
@@ -436,13 +520,14 @@ def test_beam_search(lib):
     assert all(torch.equal(x[:, :, :2], y[keep.long()][:, :, :2]) for x, y in zip(_blocks(left), _blocks(own)))
 
 
-def test_a_captured_step(lib):
+@pytest.mark.parametrize("pcap", (2048, 8192))
+def test_a_captured_step(lib, pcap):
     """Append, attend, choose and reorder in one graph, replayed between eager steps of another search that uses the same kernels."""
     P, S, Hkv, group, d, V = 2, 4, 2, 4, 64, 3000
     g = _gen(31)
     H, B = Hkv * group, P * S
-    prefix = _filled(g, P, Hkv, 2048, d, [2000, 1500])
-    prefix_lengths = _i32([2000, 1500])
+    prefix = _filled(g, P, Hkv, pcap, d, [pcap - 48, 1500])
+    prefix_lengths = _i32([pcap - 48, 1500])
     head = (0.1 * torch.randn((H * d, V), generator=g)).to(DEV)
     embed = [_bf16(g, V, h, d).to(DEV) for h in (H, Hkv, Hkv)]
 
