@@ -57,7 +57,7 @@ struct List {
 };
 struct SharedPlan {
   AttendArgs prefix;                       // the prefixes as sequences: P of them, of up to S * N queries each
-  const int* starts;                       // [P * S]: real queries of its prefix's sequences in front of this one; NULL: all are real
+  const int* starts;                       // [P * S]: real queries of its prefix's sequences in front of this one; NULL: all are taken
   int groups;                              // work-groups that the lists are shared out to: a multiple of 8, 16 at least
   bool own_split;                          // the own list is; otherwise a work-group for each of its segments follows
   List prefixes, own;
@@ -331,7 +331,10 @@ SharedForm shared_form(int P, int S, int H, int H_kv, int N, int d, int prefix_c
   f.groups = most >= room ? room : (int)most / 8 * 8;
   return f;
 }
-int unit_cost(const CacheForm& f, bool heads) { return heads ? 4 : f.KW == 4 ? 2 : f.RT == 1 ? 2 : 3; }
+// What a unit costs a work-group, roughly: with as many running as fit, the block of a segment of up to 16 rows takes 0.7 us at d = 128, of 64 rows 1.3, of 128 rows 2.0.
+// Few own segments are a matter of their chains' latency, and get twice the work-groups, or they would end after the prefixes' (16 answers about 131072 tokens:
+// 61.7 us, and 68 without; 128 beams 55.4 with it).
+int unit_cost(const CacheForm& f, bool heads, bool few) { return heads ? 4 : f.KW == 4 ? (few ? 2 : 1) : f.RT == 1 ? 2 : 3; }
 
 template <int D, int RT, int KW, int ORT, int OKW, bool HEADS> hipError_t launch_shared(const SharedArgs& a, const SharedForm& f, hipStream_t stream) {
   SharedPlan plan{};
@@ -352,29 +355,32 @@ template <int D, int RT, int KW, int ORT, int OKW, bool HEADS> hipError_t launch
   plan.prefix = p;
   plan.prefix.cache = a.prefix;
   plan.prefix.lengths = a.prefix_lengths;
-  plan.prefix.counts = p.counts ? integers + (size_t)a.P * a.S : nullptr;
+  // Padded queries are left out of a prefix's rows, for a launch that finds where the real ones begin (5 us); with one query a sequence, those that have ended are not
+  // worth it.
+  const bool padded = p.counts && p.N > 1;
+  plan.prefix.counts = padded ? integers + (size_t)a.P * a.S : nullptr;
   plan.prefix.B = a.P;
   plan.prefix.N = a.S * p.N;
   plan.prefix.causal = 0;
-  plan.starts = p.counts ? integers : nullptr;
+  plan.starts = padded ? integers : nullptr;
   plan.groups = f.groups;
   plan.own_split = f.own_split;
   plan.prefixes.heads = p.H_kv;
   plan.prefixes.tiles = f.prefix.tiles;
-  plan.prefixes.cost = unit_cost(f.prefix, false);
+  plan.prefixes.cost = unit_cost(f.prefix, false, true);
   plan.own.heads = f.own_heads;
   plan.own.tiles = f.own.tiles;
-  plan.own.cost = unit_cost(f.own, f.heads);
+  plan.own.cost = unit_cost(f.own, f.heads, f.own_segments < 256);
   const unsigned row_tiles = (unsigned)(((long long)a.S * p.N * p.group + 15) / 16);
   if (!grid_fits(row_tiles, 128)) return hipErrorInvalidConfiguration;     // (with more threads, there are fewer than 128 segments)
-  if (p.counts) {
+  if (padded) {
     attn_cache_starts_kernel<<<(unsigned)a.P, kAttendThreads, 0, stream>>>(p.counts, a.S, p.N, integers, integers + (size_t)a.P * a.S);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   attn_cache_shared_kernel<D, RT, KW, ORT, OKW, HEADS><<<(unsigned)(f.groups + (f.own_split ? 0 : f.own_segments)), kAttendThreads, 0, stream>>>(a, plan);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (f.groups > 4 * f.segments)
-    attn_cache_shared_merge_kernel<D, RT, KW, ORT, OKW, HEADS, 16, 2><<<dim3(row_tiles, (unsigned)(p.H_kv * (D / 32)), (unsigned)a.P), 1024, 0, stream>>>(a, plan);
+    attn_cache_shared_merge_kernel<D, RT, KW, ORT, OKW, HEADS, 8, 2><<<dim3(row_tiles, (unsigned)(p.H_kv * (D / 32)), (unsigned)a.P), 512, 0, stream>>>(a, plan);
   else
     attn_cache_shared_merge_kernel<D, RT, KW, ORT, OKW, HEADS, 2, D / 16><<<dim3(row_tiles, (unsigned)p.H_kv, (unsigned)a.P), 128, 0, stream>>>(a, plan);
   return hipGetLastError();

@@ -139,6 +139,7 @@ def _fill_on_gpu(seed, B, Hkv, cap, d, lengths):
     (1, 5, 2, 4, 7, 4096, 128),             # 28 rows of a sequence
     (1, 12, 8, 3, 16, 8192, 64),            # 48, and tiles of 128 of the prefix
     (2, 3, 1, 3, 45, 3200, 640),            # 135
+    (1, 33, 4, 2, 1, 9600, 128),            # one query a sequence, of some that have ended
 ])
 def test_prefixes_that_are_read_once(lib, d, P, S, Hkv, group, N, pcap, cap):
     """Every pair of forms of the two lists, with padded batches and without."""
@@ -239,6 +240,38 @@ def test_strides_outputs_workspaces_and_streams(lib, pcap):
     a = binding.attn_cache_fwd_shared(one, *args[1:])
     b = binding.attn_cache_fwd_shared(one.contiguous(), *args[1:])
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_two_calls_at_once(lib):
+    """On two streams, with workspaces of their own, and replays of two graphs in turn: each call's results are its own."""
+    calls = []
+    for seed, (P, S, N) in enumerate(((2, 24, 1), (1, 6, 9))):
+        prefix, cache = _fill_on_gpu(seed, P, 4, 8192, 64, [8000 - seed] * P), _fill_on_gpu(seed + 5, P * S, 4, 128, 64, [100 + seed] * (P * S))
+        q = torch.randn((P * S, 16, N, 64), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV).bfloat16()
+        assert binding.cache_fwd_shared_workspace_bytes(P, S, 16, 4, N, 64, 8192, 128) > 0
+        calls.append((q, prefix, _i32([8000 - seed] * P), cache, _i32([100 + seed] * (P * S)), 0.125))
+    want = [binding.attn_cache_fwd_shared(*c) for c in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for c, st in zip(calls, streams):
+            with torch.cuda.stream(st):
+                got.append(binding.attn_cache_fwd_shared(*c))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+    graphs, outs = [], []
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(binding.attn_cache_fwd_shared(*c))
+    for _ in range(4):
+        for g, out, w, c in zip(graphs, outs, want, calls):
+            out[0].zero_(), out[1].zero_()
+            g.replay()
+            again = binding.attn_cache_fwd_shared(*c)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(w, out)) and all(torch.equal(a, b) for a, b in zip(w, again))
 
 
 def test_sharing_is_what_copies_would_give(lib):
