@@ -298,6 +298,7 @@ struct SharedForm {
 // is read once.  us, joint / shared, P x S, H 32/8, d 128, own 16 to 128 tokens of 128: prefixes of 1024: 1x4 10.3 / 13.8, 1x16 10.3 / 17.1, 8x4 11.5 / 16.7,
 // 1x64 17.6 / 21.3, 4x32 32.1 / 25.7, 16x8 32.2 / 25.3;  of 2048: 1x4 15.7 / 14.8, 8x4 16.7 / 19.7, 1x64 28.1 / 22.5, 16x8 55.6 / 33.5;  of 512: 16x8 22.0 / 22.7;  S = 1:
 // 64x1 of 1024 29.2 / 43.5;  16 queries, 1x8 of 1024: 23.7 / 25.3;  64 queries, 2x4 of 2048: 58.5 / 49.9;  d 64, H 12/12: 1x4 of 2048 10.2 / 12.7, 16x8 of 1024 22.2 / 17.9.
+// One sequence a prefix (S = 1, here with own caches of 512) has nothing to share, and long batches gain nothing from parts: 16x1 of 4096 34.4 / 40.2, 64x1 of 8192 184 / 203;  8x1 of 8192 54.9 / 36.6.
 bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double P, double S, double H_kv, int d, int prefix_blocks, int blocks) {
   const double wide = d / 128.0, megabytes = 128e-6 * d, segments = P * S * H_kv * own.tiles, all = prefix_blocks + blocks;
   auto busy = [&](const CacheForm& f, double number) { return number * wide * (f.KW == 4 ? 0.7 : f.RT == 1 ? 1.3 : 2.0) / 512; };
@@ -305,7 +306,7 @@ bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double P, do
   const double once = P * H_kv * ((double)prefix_blocks + S * blocks) * megabytes;
   const double joint = 4.5 + std::max(std::max(chain, segments * all * megabytes / 10.5), std::max(once / 5.2, own.KW == 4 ? 0.0 : busy(own, segments * all)));
   const double shared = 12 + (own.KW == 4 ? 0 : 8) + wide * (1.5 + 0.006 * P * S * H_kv) +
-                        std::max(once / 6, busy(prefix, P * H_kv * prefix.tiles * prefix_blocks) + busy(own, segments * blocks));
+                        std::max(once / (S == 1 ? 5 : 6), busy(prefix, P * H_kv * prefix.tiles * prefix_blocks) + busy(own, segments * blocks));
   return joint < shared;
 }
 // Own segments of up to 16 rows have a work-group each where attn_cache_fwd's rule says so; up to four blocks, four heads have one (us, four heads / one: 16 x 8 of
