@@ -857,6 +857,8 @@ def attn_cache_fork(cache, sources, lengths, out=None, stream=None):
     if out is None:
         out = _on(device, stream, lambda: cache_empty(sources.shape[0], H_kv, capacity, d, device))
     B_out, Ho, capacity_out, do, device_out = _cache_shape(out, "out")
+    if H_kv == 0 and B_out:                # (the library does nothing then, and lengths_out would stay as it is)
+        raise ValueError("cache must have heads")
     if (B_out, Ho, do, device_out) != (sources.shape[0], H_kv, d, device):
         raise ValueError("out must have a sequence for each of sources, and the heads and head size of the cache")
     lengths_out = _on(device, stream, lambda: torch.empty((B_out,), dtype=torch.int32, device=device))
@@ -877,6 +879,8 @@ def attn_cache_reorder(cache, parents, lengths, stream=None):
     B, H_kv, capacity, d, device = _cache_shape(cache)
     if parents.dim() != 2 or parents.numel() != B:
         raise ValueError("parents must be an int32 tensor [P,S] with a value for each sequence of the cache")
+    if H_kv == 0 and B:
+        raise ValueError("cache must have heads")
     P, S = parents.shape
     _dense(parents, "parents", (P, S), torch.int32, device)
     _dense(lengths, "lengths", (B,), torch.int32, device)

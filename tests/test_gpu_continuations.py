@@ -242,6 +242,34 @@ def test_strides_outputs_workspaces_and_streams(lib, pcap):
     assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
+def test_a_prefix_beyond_32_bits(lib):
+    """A second head that begins 2^32 bytes behind the first, and tokens in the last blocks of a cache."""
+    d, cap, length = 128, 1 << 25, 130
+    small, big = _fill_on_gpu(1, 1, 2, 192, d, [length]), binding.cache_empty(1, 2, cap, d, DEV)
+    for t, u in zip(_blocks(small), _blocks(big)):
+        u[:, :, :3] = t
+    cache = _fill_on_gpu(2, 5, 2, 64, d, [9, 8, 7, 64, 1])
+    q = torch.randn((5, 6, 1, d), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).bfloat16()
+    args = (cache, _i32([9, 8, 7, 64, 1]), d ** -0.5)
+    O, lse = binding.attn_cache_fwd_shared(q, big, _i32([length]), *args)
+    _check_on_gpu(q, small, [length], cache, [9, 8, 7, 64, 1], [1] * 5, d ** -0.5, True, O, lse)
+    # all of it: weights of one huge key's block near the end decide
+    for t in big[:2]:
+        t.view(torch.uint8).zero_()
+    big.K_scale.fill_(1.0), big.V_scale.fill_(1.0)
+    big.K.view(torch.uint8)[0, :, cap - 70] = 0x7e          # 448
+    big.V.view(torch.uint8)[0, :, (cap - 70) // 64, :, (cap - 70) % 64] = 0x38          # 1
+    O, lse = binding.attn_cache_fwd_shared(q.abs(), big, _i32([cap]), *args)
+    assert (O == 1).all()
+
+
+def test_caches_without_heads_are_refused(lib):
+    c = binding.cache_empty(2, 0, 64, 64, DEV)
+    for call in (lambda: binding.attn_cache_fork(c, _i32([0]), _i32([1, 1])), lambda: binding.attn_cache_reorder(c, _i32([[1, 0]]), _i32([1, 1]))):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_two_calls_at_once(lib):
     """On two streams, with workspaces of their own, and replays of two graphs in turn: each call's results are its own."""
     calls = []
