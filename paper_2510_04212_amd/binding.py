@@ -898,7 +898,7 @@ def beam_select_workspace_bytes(B, beams, V, n):
 
 def attn_beam_select(logits, scores, n, finished=None, end_token=None, workspace=None, stream=None):
     """(parents, tokens, sums, ended), [B,n] each: the n (<= 128) continuations with the largest scores[b,k] + log_softmax(logits[b,k])[t] of each
-    item's beams, the largest first (equal ones: the lower beam, then the lower token), as int32, int32, float32 and bool.
+    item's beams, the largest first (equal ones: the lower beam, then the larger logit, then the lower token), as int32, int32, float32 and bool.
 
     logits: float32 or bfloat16 [B,beams,V] with a contiguous last dimension; scores: float32 [B,beams].  finished: bool [B,beams], beams that
     have ended: they continue with end_token alone, which adds nothing to their score.  ended: whether a continuation is, or had come to, an end.
