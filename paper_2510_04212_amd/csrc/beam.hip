@@ -8,12 +8,14 @@
 // |x - m| 2^-23, of the difference and of log2(e), and the hardware exponential's 2^-23), a thread's sum too (of up to 32 terms), everything after it float64.
 #include "beam.hpp"
 #include "cache.hpp"
-#include <algorithm>
+#include <type_traits>
 
 namespace {
 
 constexpr int kThreads = 256;
 typedef unsigned long long u64;
+typedef u32x4 __attribute__((aligned(4))) At4;
+typedef u32x4 __attribute__((aligned(2))) At2;
 
 // Larger <=> better, of one beam: by value, then by index, the lower first; -0 = +0.  0: none.
 DEVI unsigned order(float x) {
@@ -43,11 +45,10 @@ struct ScanForm {
   __host__ __device__ size_t lists_at() const { return (size_t)rows * chunks * sizeof(Stat); }
   size_t bytes(int n) const { return lists_at() + (size_t)rows * chunks * n * sizeof(u64); }
 };
-// slack: elements that a row may begin behind a 16-byte boundary
-ScanForm scan_form(int B, int beams, int V, int n, int slack) {
+ScanForm scan_form(int B, int beams, int V, int n) {
   ScanForm l;
   l.rows = (long long)B * beams;
-  auto chunks = [&](int per_thread) { return (int)(((long long)V + slack + kThreads * per_thread - 1) / (kThreads * per_thread)); };
+  auto chunks = [&](int per_thread) { return (V + kThreads * per_thread - 1) / (kThreads * per_thread); };
   l.per_thread = l.rows * V <= 1 << 22 && (long long)beams * chunks(8) * n <= 4096 ? 8 : 32;
   l.chunks = chunks(l.per_thread);
   return l;
@@ -124,27 +125,33 @@ __global__ __launch_bounds__(kThreads, 5) void attn_beam_scan_kernel(BeamArgs p,
   if (!(__builtin_fabsf(p.scores[row]) < INFINITY)) return;
   const int b = (int)(row / (unsigned)p.beams), k = (int)(row - (unsigned)(b * p.beams));
   const char* at = static_cast<const char*>(p.logits) + (b * p.stride_b + k * p.stride_beam) * SIZE;
-  // the thread's elements, 16 bytes at a time from 16-byte boundaries on
-  const int shift = (int)((reinterpret_cast<uintptr_t>(at) & 15) / SIZE), chunk0 = chunk * (kThreads * PER) - shift;       // (V <= 2^24)
-  const int first = chunk0 + tid * VEC;
+  // The thread's elements, 16 bytes at a time, by their tokens, wherever the row begins: sums in another order would be others in their last bits, and equal
+  // beams' no longer equal.  Loads of 16 bytes from any address cost nothing (32 x 8 rows of 131072 n 16: 34.2 us, and 34.3 at a pitch of 131073; bf16 26.8 and 27.9).
+  using Anywhere = std::conditional_t<WIDE, At4, At2>;
+  const int chunk0 = chunk * (kThreads * PER), first = chunk0 + tid * VEC;                 // (V <= 2^24)
   auto index = [&](int i) { return first + i / VEC * (kThreads * VEC) + i % VEC; };
   auto load = [&](int e) {
-    if (e < 0 || e >= p.V) return -INFINITY;
+    if (e >= p.V) return -INFINITY;
     return WIDE ? reinterpret_cast<const float*>(at)[e] : __uint_as_float((unsigned)reinterpret_cast<const unsigned short*>(at)[e] << 16);
   };
   float x[PER];
-  if (chunk0 >= 0 && chunk0 + kThreads * PER <= p.V) {     // a whole chunk: all loads in flight at once
+  {
     u32x4 w[LOADS];
+    const bool whole = chunk0 + kThreads * PER <= p.V;
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) w[j] = *reinterpret_cast<const u32x4*>(at + (long long)index(j * VEC) * SIZE);
+    for (int j = 0; j < LOADS; ++j) {      // all in flight at once
+      const int e = index(j * VEC);
+      if (whole || e + VEC <= p.V) w[j] = *reinterpret_cast<const Anywhere*>(at + (long long)e * SIZE);
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const unsigned bits = WIDE ? w[i / VEC][i % 4] : w[i / VEC][i % VEC / 2];
       x[i] = __uint_as_float(WIDE ? bits : (i & 1) ? bits & 0xffff0000u : bits << 16);
     }
-  } else {
+    if (!whole)                            // the row's last elements one by one (32 x 8 rows of 131000: 34.4 us, and 46.4 with the whole last chunk so)
 #pragma unroll
-    for (int i = 0; i < PER; ++i) x[i] = load(index(i));
+      for (int i = 0; i < PER; ++i)
+        if (index(i - i % VEC) + VEC > p.V) x[i] = load(index(i));
   }
   float of_load[LOADS], mine = -INFINITY;  // (maxima pass over NaN; the sum below does not)
 #pragma unroll
@@ -397,14 +404,11 @@ __global__ __launch_bounds__(kChooseThreads) void attn_beam_choose_kernel(BeamAr
 }  // namespace
 
 size_t attn_beam_select_partial_bytes(int B, int beams, int V, int n) {
-  // (with the most slack; which chunks are taken may depend on it)
-  return std::max(scan_form(B, beams, V, n, 7).bytes(n), scan_form(B, beams, V, n, 0).bytes(n));
+  return scan_form(B, beams, V, n).bytes(n);
 }
 
 hipError_t attn_beam_select_dispatch(const BeamArgs& p, hipStream_t stream) {
-  const int size = p.wide ? 4 : 2;
-  const bool aligned = (reinterpret_cast<uintptr_t>(p.logits) | (uintptr_t)(p.stride_b * size) | (uintptr_t)(p.stride_beam * size)) % 16 == 0;
-  const ScanForm l = scan_form(p.B, p.beams, p.V, p.n, aligned ? 0 : 16 / size - 1);
+  const ScanForm l = scan_form(p.B, p.beams, p.V, p.n);
   if (!grid_fits(l.rows * l.chunks, kThreads)) return hipErrorInvalidConfiguration;
   Stat* stats = static_cast<Stat*>(p.workspace);
   u64* lists = reinterpret_cast<u64*>(static_cast<char*>(p.workspace) + l.lists_at());

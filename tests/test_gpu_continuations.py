@@ -525,6 +525,26 @@ def test_select_strides_and_alignment(lib):
             x.fill_(float("nan"))
 
 
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_select_does_not_depend_on_where_rows_lie(lib, dtype):
+    """Equal beams of ordinary logits in rows that begin anywhere between two 16-byte boundaries: their sums are the same bits, so the lower beam goes first, and the
+    same values at another address or distance give the same bits."""
+    size = dtype.itemsize
+    for V, beams, n in ((4099, 8, 5), (4099, 8, 60), (50257, 8, 12), (33001, 5, 128), (200003, 8, 6)):
+        for seed in range(3):
+            row = 2.5 * torch.randn(V, generator=_gen(V + seed)).to(DEV)
+            x = row.to(dtype).repeat(1, beams, 1)
+            assert len({x[0, k].data_ptr() % 16 for k in range(beams)}) == min(beams, 16 // size)
+            scores = torch.full((1, beams), -3.7, device=DEV)
+            want = _select(x, scores, n, label=f"{V} {n} {seed}")
+            for first, pitch in ((0, -(-V // 64) * 64), (1, V), (3, V + 2), (7, V + 13)):
+                room = torch.full((first + beams * pitch,), float("nan"), dtype=dtype, device=DEV)
+                y = room[first:].view(1, beams, pitch)[:, :, :V]
+                y.copy_(x)
+                got = binding.attn_beam_select(y, scores, n)
+                assert all(torch.equal(a, b) for a, b in zip(want, got)), (V, n, seed, first, pitch)
+
+
 def test_select_on_a_stream_with_a_workspace(lib):
     g = _gen(12)
     x, s = torch.randn((4, 4, 9000), generator=g).to(DEV), torch.zeros((4, 4), device=DEV)
