@@ -1,6 +1,7 @@
 // Attention of sequences that continue prefixes they share with others (attn_cache_fwd_shared of include/attn.h).
 #include "cache_attend.hpp"
 #include <algorithm>
+#include <cmath>
 
 namespace {
 
@@ -294,19 +295,26 @@ struct SharedForm {
   size_t slot_floats_own(int d) const { return heads ? 4 * (size_t)(d / 16 * 256 + 32) : own.slot_floats(d); }
 };
 // Estimates in us, from capacities.  Joint: one launch, bound by a segment's chain of blocks, by all segments' reads through the caches (10.5 TB/s), by
-// what has to come from memory (5.2), or by the vector and matrix units.  Shared: finding the work, parts and a second launch cost 12 us and more, and then a prefix
-// is read once.  us, joint / shared, P x S, H 32/8, d 128, own 16 to 128 tokens of 128: prefixes of 1024: 1x4 10.3 / 13.8, 1x16 10.3 / 17.1, 8x4 11.5 / 16.7,
-// 1x64 17.6 / 21.3, 4x32 32.1 / 25.7, 16x8 32.2 / 25.3;  of 2048: 1x4 15.7 / 14.8, 8x4 16.7 / 19.7, 1x64 28.1 / 22.5, 16x8 55.6 / 33.5;  of 512: 16x8 22.0 / 22.7;  S = 1:
-// 64x1 of 1024 29.2 / 43.5;  16 queries, 1x8 of 1024: 23.7 / 25.3;  64 queries, 2x4 of 2048: 58.5 / 49.9;  d 64, H 12/12: 1x4 of 2048 10.2 / 12.7, 16x8 of 1024 22.2 / 17.9.
-// One sequence a prefix (S = 1, here with own caches of 512) has nothing to share, and long batches gain nothing from parts: 16x1 of 4096 34.4 / 40.2, 64x1 of 8192 184 / 203;  8x1 of 8192 54.9 / 36.6.
-bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double P, double S, double H_kv, int d, int prefix_blocks, int blocks) {
+// what has to come from memory (5.2; 6.2 where one work-group reads it), or by the vector and matrix units.  Shared: finding the work, parts and a second launch cost
+// 12 us and more, and then a prefix is read once.  us, joint / shared, P x S, H 32/8, d 128, own 16 to 128 tokens of 128: prefixes of 1024: 1x4 10.3 / 13.8, 1x16 10.3 / 17.1,
+// 8x4 11.5 / 16.7, 1x64 17.6 / 21.3, 4x32 32.1 / 25.7, 16x8 32.2 / 25.3;  of 2048: 1x4 15.7 / 14.8, 8x4 16.7 / 19.7, 1x64 28.1 / 22.5, 16x8 55.6 / 33.5;  of 512: 16x8 22.0 / 22.7;
+// 16 queries, 1x8 of 1024: 23.7 / 25.3;  64 queries, 2x4 of 2048: 58.5 / 49.9;  d 64, H 12/12: 1x4 of 2048 10.2 / 12.7, 16x8 of 1024 22.2 / 17.9.
+// S = 1, 2, own capacity 256, full prefixes: of 4096: 16x1 27.5 / 36.0, 64x1 96.9 / 116, 8x2 27.4 / 22.8, 64x2 120 / 125;  64 queries each: 64x1 324 / 402.
+//
+// What the estimates do not know is how long the prefixes are: where one is full and the others are short, the joint form takes its chain all the same.  So that
+// may be up to twice what the shared form costs beside its bytes.  One full prefix among 500 tokens each / all full: 16x1 of 131072 694 / 70 and 840 / 704, of 8192 48.1 / 24.6 and
+// 52.5 / 56.1;  128x1 of 8192 70.1 / 48.5 and 359 / 384, of 4096 49.8 / 47.1 and 189 / 213;  16 queries, 64x1 of 8192 146 / 49.9 and 236 / 259;  d 32, H 16/8, 16x1 of 32768 64.5 / 18.9 and
+// 94.5 / 49.4;  16 queries of it, 16x1 of 8192 72.1 / 17.8 and 73.5 / 33.8 (small blocks take longer than their bytes).
+bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double rows, double P, double S, double H_kv, int d, int prefix_blocks, int blocks) {
   const double wide = d / 128.0, megabytes = 128e-6 * d, segments = P * S * H_kv * own.tiles, all = prefix_blocks + blocks;
   auto busy = [&](const CacheForm& f, double number) { return number * wide * (f.KW == 4 ? 0.7 : f.RT == 1 ? 1.3 : 2.0) / 512; };
-  const double chain = all * wide * (own.KW == 4 ? 0.33 : own.RT == 1 ? 1.05 : 1.6);
+  const double chain = all * (own.KW == 4 ? std::max(0.33 * wide, 0.115) : own.RT == 1 ? 0.4 + 0.65 * wide : 0.6 + wide);
+  const double begin = 12 + (own.KW == 4 ? 0 : 8) + wide * (1.5 + 0.006 * P * S * H_kv * std::ceil(rows / 16));        // parts of 16 rows: 32 KB through memory
+  if (chain > 2 * begin) return false;
   const double once = P * H_kv * ((double)prefix_blocks + S * blocks) * megabytes;
-  const double joint = 4.5 + std::max(std::max(chain, segments * all * megabytes / 10.5), std::max(once / 5.2, own.KW == 4 ? 0.0 : busy(own, segments * all)));
-  const double shared = 12 + (own.KW == 4 ? 0 : 8) + wide * (1.5 + 0.006 * P * S * H_kv) +
-                        std::max(once / (S == 1 ? 5 : 6), busy(prefix, P * H_kv * prefix.tiles * prefix_blocks) + busy(own, segments * blocks));
+  const double joint =
+      4.5 + std::max(std::max(chain, segments * all * megabytes / 10.5), std::max(once / (S == 1 ? 6.2 : 5.2), own.KW == 4 ? 0.0 : busy(own, segments * all)));
+  const double shared = begin + std::max(once / 6, busy(prefix, P * H_kv * prefix.tiles * prefix_blocks) + busy(own, segments * blocks));
   return joint < shared;
 }
 // Own segments of up to 16 rows have a work-group each where attn_cache_fwd's rule says so; up to four blocks, four heads have one (us, four heads / one: 16 x 8 of
@@ -324,7 +332,7 @@ SharedForm shared_form(int P, int S, int H, int H_kv, int N, int d, int prefix_c
   f.segments = (long long)P * H_kv * f.prefix.tiles;
   f.own_segments = (long long)P * S * f.own_heads * f.own.tiles;
   f.own_split = f.own.split || f.own.KW == 1 || f.own_segments > 1 << 20;
-  f.shared = f.own.tiles > 65535 || !joint_is_faster(f.prefix, f.own, P, S, H_kv, d, prefix_capacity / kBlock, capacity / kBlock);
+  f.shared = f.own.tiles > 65535 || !joint_is_faster(f.prefix, f.own, (double)rows, P, S, H_kv, d, prefix_capacity / kBlock, capacity / kBlock);
   auto shares = [&](const CacheForm& form, bool heads, int B, int H_kv, int capacity) {
     return cache_units(B, H_kv, form, capacity, heads ? kHeadsStart : kStart) / (heads ? kLeast<1, true> : form.KW == 4 ? kLeast<4, false> : kLeast<1, false>);
   };

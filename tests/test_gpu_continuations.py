@@ -168,6 +168,20 @@ def test_prefixes_that_are_read_once(lib, d, P, S, Hkv, group, N, pcap, cap):
         _check_on_gpu(q, prefix, [0], full, [min(max(w, 0), cap) for w in wild], [[N, N, 0][i % 3] for i in range(P * S)], d ** -0.5, False, O, lse, "wild")
 
 
+@pytest.mark.parametrize("P,S,group,Hkv,N,d,pcap", [(16, 1, 4, 2, 1, 128, 32768), (6, 2, 1, 3, 1, 64, 65536), (5, 1, 2, 2, 9, 96, 16384), (9, 1, 3, 1, 30, 32, 32768)])
+def test_one_long_prefix_among_short_ones(lib, P, S, group, Hkv, N, d, pcap):
+    """Hardly any sequence shares its prefix, and one prefix is long: it is read in parts."""
+    assert binding.cache_fwd_shared_workspace_bytes(P, S, group * Hkv, Hkv, N, d, pcap, 128) > 0
+    prefix_lengths = _some(P, P, 1, 300)
+    prefix_lengths[P // 2] = pcap - 3
+    lengths = [min(128, N + x) for x in _some(N, P * S, 0, 128)]
+    prefix, cache = _fill_on_gpu(S, P, Hkv, pcap, d, prefix_lengths), _fill_on_gpu(N, P * S, Hkv, 128, d, lengths)
+    q = torch.randn((P * S, group * Hkv, N, d), generator=torch.Generator(device=DEV).manual_seed(d), device=DEV).bfloat16()
+    for counts in (None, [N - i % (N + 1) for i in range(P * S)]):
+        O, lse = binding.attn_cache_fwd_shared(q, prefix, _i32(prefix_lengths), cache, _i32(lengths), d ** -0.5, True, None if counts is None else _i32(counts))
+        _check_on_gpu(q, prefix, prefix_lengths, cache, lengths, [N] * (P * S) if counts is None else counts, d ** -0.5, True, O, lse, f"{counts is None}")
+
+
 @pytest.mark.parametrize("N", (1, 7, 30))
 def test_lengths_at_their_ends(lib, N):
     """Empty prefixes, empty caches, queries without tokens of their own, padded sequences, all together; and lengths that no cache has."""

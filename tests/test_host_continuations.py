@@ -61,6 +61,16 @@ def test_shared_attention_refusals(binding):
     assert binding.cache_fwd_shared_workspace_bytes(0, 4, 4, 2, 1, 64, 64, 64) == 0 == binding.cache_fwd_shared_workspace_bytes(1, 4, 3, 2, 1, 64, 64, 64)
 
 
+def test_long_prefixes_are_shared_out(binding):
+    """A work-group that walks a long prefix alone ends long after the others where these are short: such calls have parts, and so a workspace, however little the
+    sequences share."""
+    for P in (1, 4, 16, 64):
+        for S in (1, 2, 3):
+            for H, Hkv, d, N in ((32, 8, 128, 1), (12, 12, 64, 1), (16, 8, 32, 1), (8, 4, 256, 1), (32, 8, 128, 16), (16, 8, 32, 16), (32, 8, 128, 64), (8, 1, 128, 2)):
+                for pcap in (1 << 15, 1 << 17, 1 << 20):
+                    assert binding.cache_fwd_shared_workspace_bytes(P, S, H, Hkv, N, d, pcap, 512) > 0, (P, S, H, Hkv, N, d, pcap)
+
+
 def test_fork_refusals(binding):
     lib = binding.raw()
     names = ["K", "V", "Ks", "Vs", "sources", "lengths", "Ko", "Vo", "Kso", "Vso", "lo"]
