@@ -332,7 +332,7 @@ SharedForm shared_form(int P, int S, int H, int H_kv, int N, int d, int prefix_c
   f.segments = (long long)P * H_kv * f.prefix.tiles;
   f.own_segments = (long long)P * S * f.own_heads * f.own.tiles;
   f.own_split = f.own.split || f.own.KW == 1 || f.own_segments > 1 << 20;
-  f.shared = f.own.tiles > 65535 || !joint_is_faster(f.prefix, f.own, (double)rows, P, S, H_kv, d, prefix_capacity / kBlock, capacity / kBlock);
+  f.shared = !joint_is_faster(f.prefix, f.own, (double)rows, P, S, H_kv, d, prefix_capacity / kBlock, capacity / kBlock);
   auto shares = [&](const CacheForm& form, bool heads, int B, int H_kv, int capacity) {
     return cache_units(B, H_kv, form, capacity, heads ? kHeadsStart : kStart) / (heads ? kLeast<1, true> : form.KW == 4 ? kLeast<4, false> : kLeast<1, false>);
   };

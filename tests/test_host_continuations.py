@@ -71,6 +71,17 @@ def test_long_prefixes_are_shared_out(binding):
                     assert binding.cache_fwd_shared_workspace_bytes(P, S, H, Hkv, N, d, pcap, 512) > 0, (P, S, H, Hkv, N, d, pcap)
 
 
+def test_more_row_tiles_than_a_grid_has_are_refused(binding):
+    """Tiles of 128 rows are the grid's second dimension in the form without parts; the other form is not asked for more either."""
+    null = [None] * 4
+    for P, S in ((1, 1), (1, 2), (2, 1)):
+        for pcap in (64, 8192):
+            size = lambda N: (P, S, 1, 1, N, 64, pcap, 64)
+            refused = lambda N: binding.raw().attn_cache_fwd_shared(None, None, *null, None, *null, None, None, None, None, None, 0, *size(N), 1, 0.125, None)
+            assert refused(65535 * 128) == NULL and refused(65535 * 128 + 1) == UNSUP
+            assert binding.cache_fwd_shared_workspace_bytes(*size(65535 * 128 + 1)) == 0
+
+
 def test_fork_refusals(binding):
     lib = binding.raw()
     names = ["K", "V", "Ks", "Vs", "sources", "lengths", "Ko", "Vo", "Kso", "Vso", "lo"]
