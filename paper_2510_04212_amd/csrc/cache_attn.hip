@@ -8,7 +8,96 @@ namespace {
 
 constexpr int kThreads = kAttendThreads;
 
-// SPLIT: shares of the list of blocks; otherwise one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
+// Many rows whose segments are whole, of 32 blocks at most (cache_form): attend's loop over staged blocks with nothing to share out or to join, and a segment's scales in
+// one load.  2048 queries of 4 sequences of 2048 tokens, H 16/8, d 32 and 64, 32/8, 96 and 128, 16/4, 256: 70.0, 70.3, 152, 171 and 259 us, and 73.2, 74.1, 155, 178 and 264
+// as an instance of attend.
+template <int D, int RT>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_whole_kernel(AttendArgs p, int tiles) {
+  constexpr int M = 64 * RT;
+  __shared__ __attribute__((aligned(1024))) char staged[2 * Staged<D>::kBytes];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const Problem q{p.lengths, p.counts, p.cache.capacity, p.N, p.group, p.causal, tiles, M};
+  const int nb = p.cache.capacity / kBlock;
+  const float scale_log2 = p.scale * kLog2e;
+  const int b = blockIdx.z, h = blockIdx.x, t = blockIdx.y, first_row = t * M + wave * RT * 16;
+  // (the compiler knows nothing of a copy's range, and orders the loop less well then: d 256 259 us, and 262 with the copy alone)
+  const int counted = q.blocks(b, t), blocks = max(min(counted, uniform(counted)), 0);
+  const size_t bh = (size_t)b * p.H_kv + h;
+  const unsigned char* K = p.cache.K + bh * p.cache.capacity * D;
+  const unsigned char* V = p.cache.V + bh * p.cache.capacity * D;
+  const float* Ks = p.cache.K_scale + bh * nb;
+  const float* Vs = p.cache.V_scale + bh * nb;
+  int least = 0x7fffffff, limit[RT];
+  bf16x8 qf[RT][D / 32];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const Row x = find_row(p, b, first_row + rt * 16 + r);
+    limit[rt] = x.limit;
+    least = min(least, x.limit);
+    const unsigned short* from = p.Q.at + b * p.Q.sb + (h * p.group + x.head) * p.Q.sh + x.query * p.Q.sn;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) qf[rt][c] = *reinterpret_cast<const bf16x8*>(from + query_column<D>(c, g));
+  }
+#pragma unroll
+  for (int i = 1; i < 16; i <<= 1) least = min(least, __shfl_xor(least, i));
+  least = uniform(least);
+
+  Acc<D, RT> a;
+  a.clear();
+  constexpr int MINE = Staged<D>::PIECES / 4;              // a wave fetches every fourth piece
+  const unsigned buffers = uniform(lds_address(staged));
+  unsigned from[MINE];
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) from[i] = Staged<D>::source(wave + 4 * i, lane);
+  auto fetch = [&](int blk, int buffer) {
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      const int piece = wave + 4 * i;
+      fetch_piece((piece < Staged<D>::KP ? K : V) + (size_t)blk * (kBlock * D), from[i], buffers + buffer * Staged<D>::kBytes + piece * 1024);
+    }
+  };
+  const int in_piece = r * 64 + ((g ^ slot_mask(r >> 2)) << 4), in_odd = r * 32 + g * 8;
+  const bool rows_here = first_row < p.N * p.group;
+  float k_scales = 0.f, v_scales = 0.f;    // one block's in each lane
+  if (blocks > 0) {
+    fetch(0, 0);
+    k_scales = Ks[min(lane, nb - 1)];
+    v_scales = Vs[min(lane, nb - 1)];
+    settle(k_scales);
+    settle(v_scales);
+  }
+  // what the compiler has loaded is settled in front of the loop, as in attend
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) settle(qf[rt][c]);
+  KCodes<D> k;
+  int buffer = 0;
+  for (int blk = 0; blk < blocks; ++blk) {
+    wait_vmem();
+    __syncthreads();                                       // this block has landed for all waves, and all have read the one before
+    if (blk + 1 < blocks) fetch(blk + 1, buffer ^ 1);
+    if (rows_here) {
+      const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), blk));
+      const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), blk));
+      const int base = (int)buffers + buffer * Staged<D>::kBytes;
+      VCodes<D> v;
+      read_staged<D>(k, base + in_piece, base + in_odd);
+      block_step<D, RT>(a, qf, k, v, ks, vs, scale_log2, limit, blk * kBlock + kBlock > least, blk * kBlock, g,
+                        [&] { read_staged<D>(v, base + in_piece); });
+    }
+    buffer ^= 1;
+  }
+  a.join_groups();
+  auto put = [&](int tile, const f32x4* o, float m, float l) {
+    store_row<D / 16>(p, find_row(p, b, t * M + tile * 16 + r), b, h, o, m, l, 0, g);
+  };
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) put(wave * RT + rt, a.o[rt], a.m[rt], a.l[rt]);
+}
+
+// SPLIT: shares of the list of blocks; otherwise (up to 16 rows) one segment per work-group (blockIdx: head, tile, sequence), nothing to merge.
 template <int D, int RT, int KW, bool SPLIT>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_cache_fwd_kernel(AttendArgs p, int tiles, int most_shares, bool notes_by_segment) {
   __shared__ __attribute__((aligned(1024))) char staged[kAttendBytes<D, RT, KW>];
@@ -117,7 +206,9 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_merge_kernel(AttendArgs p,
 
 template <int D, int RT, int KW> hipError_t launch_fwd(const AttendArgs& p, const CacheForm& f, hipStream_t stream) {
   if (!f.split) {
-    attn_cache_fwd_kernel<D, RT, KW, false><<<dim3((unsigned)p.H_kv, (unsigned)f.tiles, (unsigned)p.B), kThreads, 0, stream>>>(p, f.tiles, 0, false);
+    const dim3 grid((unsigned)p.H_kv, (unsigned)f.tiles, (unsigned)p.B);
+    if constexpr (KW == 1) attn_cache_whole_kernel<D, RT><<<grid, kThreads, 0, stream>>>(p, f.tiles);
+    else attn_cache_fwd_kernel<D, RT, KW, false><<<grid, kThreads, 0, stream>>>(p, f.tiles, 0, false);
     return hipGetLastError();
   }
   attn_cache_fwd_kernel<D, RT, KW, true><<<(unsigned)((f.shares + 7) / 8 * 8), kThreads, 0, stream>>>(p, f.tiles, f.shares, f.many_parts);

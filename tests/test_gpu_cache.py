@@ -729,6 +729,20 @@ def test_parts_joined_by_two_waves(lib, d, B, Hkv, group, N, cap):
 
 
 @pytest.mark.parametrize("d", DIMS)
+@pytest.mark.parametrize("N,cap", [(20, 2048), (40, 2048), (20, 64), (40, 1024)])          # 40 rows: one row tile a wave; 80: two
+def test_whole_segments_of_shared_blocks(lib, d, N, cap):
+    """A work-group for each of 512 segments of up to 32 blocks; empty ones, ends inside a block and padded sequences among them."""
+    B, Hkv, group = 64, 8, 2
+    lengths = [min(cap, (cap, 0, 1, 63, cap - 1, 65, b * 977 % cap)[b % 7]) for b in range(B)]
+    counts = [min(l, (N, N - 7, 1)[b % 3]) for b, l in enumerate(lengths)]
+    c = _filled_on_gpu(d + N, B, Hkv, cap, d, lengths)
+    assert binding.cache_fwd_workspace_bytes(B, group * Hkv, Hkv, N, d, cap) == 0
+    q = _bf16(_gen(N + d), B, group * Hkv, N, d).to(DEV)
+    O, lse = binding.attn_cache_fwd(q, c, _i32(lengths), d ** -0.5, counts=_i32(counts))
+    _check_rows(q, c, lengths, counts, d ** -0.5, O, lse, [(b, h) for b in (*range(0, 14), 34, 63) for h in (0, 5)], 16 * 32)
+
+
+@pytest.mark.parametrize("d", DIMS)
 @pytest.mark.parametrize("N", (20, 40))                    # 40 rows: one row tile a wave; 80: two
 def test_more_than_64_staged_blocks_of_a_segment(lib, d, N):
     """72 full segments of 512 blocks on 512 work-groups (256 at d = 256): 72 blocks or more each, whose scales come 64 at a time."""

@@ -175,3 +175,13 @@ def test_the_form_covers_the_rows_and_the_workspace_is_what_the_library_says(tmp
         kinds.add((RT, KW, bool(split)))
         many_parts.add((RT, KW, bool(many)))
     assert kinds == many_parts == {(RT, KW, s) for RT, KW in ((1, 4), (1, 1), (2, 1)) for s in (False, True)}
+
+
+def test_whole_segments_of_shared_blocks_are_short(tmp_path_factory):
+    """One lane of a wave holds a block's scales there: a whole segment of more than 16 rows has at most 32 blocks, however many segments there are."""
+    exe = _build(tmp_path_factory, FORMS)
+    cases = [(B, Hkv * g, Hkv, N, d, cap) for B in (1, 60, 65535) for Hkv in (1, 8, 64) for g in (1, 4) for N in (5, 17, 70, 5000) for d in (32, 128, 256)
+             for cap in (1024, 2048, 2112, 4096, 8192, 1 << 20) if B * Hkv * N < 1 << 24]
+    out = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in cases), check=True, capture_output=True, text=True).stdout
+    whole = [c[5] for c, line in zip(cases, out.splitlines()) if line.split()[1] == "1" and line.split()[4] == "0"]
+    assert max(whole) == 32 * 64
