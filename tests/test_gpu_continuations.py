@@ -168,6 +168,52 @@ def test_prefixes_that_are_read_once(lib, d, P, S, Hkv, group, N, pcap, cap):
         _check_on_gpu(q, prefix, [0], full, [min(max(w, 0), cap) for w in wild], [[N, N, 0][i % 3] for i in range(P * S)], d ** -0.5, False, O, lse, "wild")
 
 
+@pytest.mark.parametrize("d", (64, 128, 256))
+@pytest.mark.parametrize("P,S,Hkv,group,N,pcap,cap", [
+    (4, 2, 5, 3, 1, 8192, 192),             # own heads four to a work-group
+    (4, 40, 3, 1, 1, 4096, 448),            # segments of a work-group each
+    (4, 3, 3, 2, 2, 4096, 3200),            # shared out
+    (4, 12, 8, 3, 16, 8192, 64),            # 48 rows of a sequence
+    (4, 3, 1, 3, 45, 3200, 640),            # 135
+])
+def test_lengths_that_no_prefix_has(lib, d, P, S, Hkv, group, N, pcap, cap):
+    """Lengths beyond a prefix's cache are the cache's, negative ones none, for prefixes that are read once."""
+    assert binding.cache_fwd_shared_workspace_bytes(P, S, group * Hkv, Hkv, N, d, pcap, cap) > 0
+    prefix, cache = _fill_on_gpu(S, P, Hkv, pcap, d, [pcap] * P), _fill_on_gpu(N, P * S, Hkv, cap, d, [cap] * (P * S))
+    q = torch.randn((P * S, group * Hkv, N, d), generator=torch.Generator(device=DEV).manual_seed(d), device=DEV).bfloat16()
+    wild = [(2 ** 31 - 1, -7, cap, cap + 1, -2 ** 31)[i % 5] for i in range(P * S)]
+    counts = [(N + 9, 2 ** 31 - 1, -1, N)[i % 4] for i in range(P * S)]
+    (Kp, Vp), (K, V) = _values_on_gpu(prefix), _values_on_gpu(cache)
+    alpha = d ** -0.5
+    for prefix_lengths in ([2 ** 31 - 1, -1, pcap + 1, pcap - 70], [-2 ** 31, pcap + 64, 0, 2 ** 31 - 1]):
+        for c, causal in ((None, False), (counts, False), (counts, True)):
+            O, lse = binding.attn_cache_fwd_shared(q, prefix, _i32(prefix_lengths), cache, _i32(wild), alpha, causal, None if c is None else _i32(c))
+            for b in range(P * S) if P * S <= 24 else (0, 1, 2, 3, 4, S, S + 1, 2 * S - 1, 3 * S, P * S - 1):
+                n = min(max(c[b], 0), N) if c else N
+                before, own = min(max(prefix_lengths[b // S], 0), pcap), min(max(wild[b], 0), cap)
+                # query i sees positions up to length - n + i, whatever the length, of those that the cache has
+                seen = torch.tensor([min(own, max(0, wild[b] - n + i + 1)) if causal else own for i in range(n)], device=DEV)
+                for h in range(Hkv):
+                    rows = slice(h * group, (h + 1) * group)
+                    assert (O[b, rows, n:] == 0).all() and torch.isneginf(lse[b, rows, n:]).all(), (b, h)
+                    none = (before + seen == 0).expand(group, n) if n else seen.expand(group, 0) > 0
+                    o_got, l_got = O[b, rows, :n].double(), lse[b, rows, :n].double()
+                    assert (o_got[none] == 0).all() and torch.isneginf(l_got[none]).all(), (b, h)
+                    if none.all():
+                        continue
+                    k, v = torch.cat((Kp[b // S, h, :before], K[b, h, :own])), torch.cat((Vp[b // S, h, :before], V[b, h, :own]))
+                    x = q[b, rows, :n].double().reshape(-1, d)
+                    s = alpha * (x @ k.t())
+                    e = 2 * (d + 4) * 2.0 ** -24 * alpha * (x.abs() @ k.abs().t()).amax(1) + 2.0 ** -22 * s.abs().amax(1) + 2.0 ** -16
+                    s = s.view(group, n, -1).masked_fill(torch.arange(before + own, device=DEV) >= before + seen[:, None], -float("inf")).view(group * n, -1)
+                    l, p = torch.logsumexp(s, 1), torch.softmax(s, 1)
+                    real = ~none.reshape(-1)
+                    assert ((l_got.reshape(-1) - l).abs() <= e)[real].all(), (b, h, prefix_lengths, causal)
+                    o = p @ v
+                    tol = 2.0 ** -8 * o.abs() + (2.0 ** -8 + e[:, None]) * 1.01 * (p @ v.abs() + o.abs())
+                    assert ((o_got.reshape(-1, d) - o).abs() <= tol)[real].all(), (b, h, prefix_lengths, causal)
+
+
 @pytest.mark.parametrize("P,S,group,Hkv,N,d,pcap", [(16, 1, 4, 2, 1, 128, 32768), (6, 2, 1, 3, 1, 64, 65536), (5, 1, 2, 2, 9, 96, 16384), (9, 1, 3, 1, 30, 32, 32768)])
 def test_one_long_prefix_among_short_ones(lib, P, S, group, Hkv, N, d, pcap):
     """Hardly any sequence shares its prefix, and one prefix is long: it is read in parts."""
