@@ -902,8 +902,9 @@ def attn_beam_select(logits, scores, n, finished=None, end_token=None, workspace
 
     logits: float32 or bfloat16 [B,beams,V] with a contiguous last dimension; scores: float32 [B,beams].  finished: bool [B,beams], beams that
     have ended: they continue with end_token alone, which adds nothing to their score.  ended: whether a continuation is, or had come to, an end.
-    Logits of -infinity are never chosen; a beam with a NaN or +infinity, or whose score is not finite, has no continuation.  Where there are fewer
-    than n, the rest of parents and tokens is -1, and of the sums -infinity."""
+    Logits of -infinity are never chosen; masks of a finite value are candidates, and where many are equal the choice takes many times as long.  A beam
+    with a NaN or +infinity, or whose score is not finite, has no continuation.  Where there are fewer than n, the rest of parents and tokens is -1, and
+    of the sums -infinity."""
     if workspace is None and stream is None:
         out = _operators.beam_select(logits, scores, n, finished, end_token)
         if out is not None:

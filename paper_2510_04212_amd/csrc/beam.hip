@@ -88,7 +88,8 @@ template <int BITS, int EACH> DEVI unsigned reached_by(const unsigned (&x)[EACH]
 
 // Few are chosen of many, so most are left out at once: the n-th largest of the maxima of 64 or 256 groups of elements is a bound that the n best
 // reach, and hardly any others (64 groups, n = 16: 18 elements).  Those that do are gathered in LDS, and each finds its place by counting the better ones.
-// Where too many reach it (equal values), the best is taken n times.
+// Where too many reach it, the best is taken n times: equal values, or, as the bound has 16 bits (a bf16 step), many logits far from 0 together (32 x 8 x 131072, n 16:
+// 32 us; 192 with 1000 added to all; 491 with all but one in 1000 at -10000).
 //
 // Bound by bytes for large rows of float32 (32 x 8 x 131072, n 16: 27.3 us, 4.9 TB/s; 181 with the best taken n times), by the work on a chunk beside them
 // otherwise (the same in bf16: 17.9 us, 3.7 TB/s).  Without exponentials it takes as long, without the search for the best 25 and 13.

@@ -48,6 +48,10 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attn_cache_j
 // own.  Every segment leaves its rows' sums, whole or in parts, for the joining kernel.  The prefixes' are shared out to work-groups as in
 // attn_cache_fwd, to as many of those that run at once as what their units cost against the own ones' says; own ones have a work-group each, or, where they are
 // long, are shared out to the rest.
+//
+// Bound by bytes up to 64 rows (128 beams of 16 prompts: 47 us, 3.9 TB/s with 12 us of finding work and parts), by the matrix and vector units above (16 answers about 131072
+// tokens: 51.7 us, 660 TFLOP/s), where with 128-row tiles at d = 128 both lists' state does not fit beside attend's: 14 vector registers and some 400 scalar ones spill, 24 and 513
+// where own tiles have 128 rows, too (64 queries each of 2 x 8: 89 us, 690 TFLOP/s); a plain call's kernel spills 7 and 258 and reaches 1070.
 struct List {
   Join* notes;                             // one for each segment
   float* slots;                            // parts of segments: two for each work-group
@@ -319,7 +323,7 @@ bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double rows,
 }
 // Own segments of up to 16 rows have a work-group each where attn_cache_fwd's rule says so; up to four blocks, four heads have one (us, four heads / one: 16 x 8 of
 // 1024, own 128: 25.3 / 29.5; of 4096, own 512: 58 / 55.5).  More rows are shared out (64 queries each of 2 x 8, prefixes of 8192, own 1024: 108 us, and 124 whole).
-// Prefixes of more than 64 rows: two row tiles a wave where a share has ten blocks or so (256 rows of 8192: 39.8 us, and 31.9 with one; 128 of 131072: 61 and 66).
+// Prefixes of more than 64 rows: two row tiles a wave where a share has ten blocks or so (256 rows of 8192: 39.8 us, and 31.9 with one; 128 of 131072: 60 and 66).
 SharedForm shared_form(int P, int S, int H, int H_kv, int N, int d, int prefix_capacity, int capacity) {
   SharedForm f;
   const long long rows = (long long)N * (H / H_kv);
@@ -342,7 +346,7 @@ SharedForm shared_form(int P, int S, int H, int H_kv, int N, int d, int prefix_c
 }
 // What a unit costs a work-group, roughly: with as many running as fit, the block of a segment of up to 16 rows takes 0.7 us at d = 128, of 64 rows 1.3, of 128 rows 2.0.
 // Few own segments are a matter of their chains' latency, and get twice the work-groups, or they would end after the prefixes' (16 answers about 131072 tokens:
-// 61.7 us, and 68 without; 128 beams 55.4 with it).
+// 59.8 us, and 64.8 without).
 int unit_cost(const CacheForm& f, bool heads, bool few) { return heads ? 4 : f.KW == 4 ? (few ? 2 : 1) : f.RT == 1 ? 2 : 3; }
 
 template <int D, int RT, int KW, int ORT, int OKW, bool HEADS> hipError_t launch_shared(const SharedArgs& a, const SharedForm& f, hipStream_t stream) {
