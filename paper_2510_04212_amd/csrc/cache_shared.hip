@@ -306,15 +306,16 @@ struct SharedForm {
 // S = 1, 2, own capacity 256, full prefixes: of 4096: 16x1 27.5 / 36.0, 64x1 96.9 / 116, 8x2 27.4 / 22.8, 64x2 120 / 125;  64 queries each: 64x1 324 / 402.
 //
 // What the estimates do not know is how long the prefixes are: where one is full and the others are short, the joint form takes its chain all the same.  So that
-// may be up to twice what the shared form costs beside its bytes.  One full prefix among 500 tokens each / all full: 16x1 of 131072 694 / 70 and 840 / 704, of 8192 48.1 / 24.6 and
-// 52.5 / 56.1;  128x1 of 8192 70.1 / 48.5 and 359 / 384, of 4096 49.8 / 47.1 and 189 / 213;  16 queries, 64x1 of 8192 146 / 49.9 and 236 / 259;  d 32, H 16/8, 16x1 of 32768 64.5 / 18.9 and
-// 94.5 / 49.4;  16 queries of it, 16x1 of 8192 72.1 / 17.8 and 73.5 / 33.8 (small blocks take longer than their bytes).
+// may be up to twice what the shared form costs beside its bytes, where there is more than one prefix (a single one of 4096, 4 x 512 queries: 171 / 190).  One full prefix among
+// 500 tokens each, and all full: 16x1 of 131072 694 / 70 and 840 / 704, of 8192 48.1 / 24.6 and 52.5 / 56.1;  128x1 of 8192 70.1 / 48.5 and 359 / 384, of 4096 49.8 / 47.1 and
+// 189 / 213;  16 queries, 64x1 of 8192 146 / 49.9 and 236 / 259;  256 queries, 16x1 of 8192 248 / 162 and 563 / 657;  d 32, H 16/8, 16x1 of 32768 64.5 / 18.9 and 94.5 / 49.4;
+// 16 queries of it, 16x1 of 8192 72.1 / 17.8 and 73.5 / 33.8 (small blocks take longer than their bytes).
 bool joint_is_faster(const CacheForm& prefix, const CacheForm& own, double rows, double P, double S, double H_kv, int d, int prefix_blocks, int blocks) {
   const double wide = d / 128.0, megabytes = 128e-6 * d, segments = P * S * H_kv * own.tiles, all = prefix_blocks + blocks;
   auto busy = [&](const CacheForm& f, double number) { return number * wide * (f.KW == 4 ? 0.7 : f.RT == 1 ? 1.3 : 2.0) / 512; };
   const double chain = all * (own.KW == 4 ? std::max(0.33 * wide, 0.115) : own.RT == 1 ? 0.4 + 0.65 * wide : 0.6 + wide);
   const double begin = 12 + (own.KW == 4 ? 0 : 8) + wide * (1.5 + 0.006 * P * S * H_kv * std::ceil(rows / 16));        // parts of 16 rows: 32 KB through memory
-  if (chain > 2 * begin) return false;
+  if (P > 1 && chain > 2 * begin) return false;
   const double once = P * H_kv * ((double)prefix_blocks + S * blocks) * megabytes;
   const double joint =
       4.5 + std::max(std::max(chain, segments * all * megabytes / 10.5), std::max(once / (S == 1 ? 6.2 : 5.2), own.KW == 4 ? 0.0 : busy(own, segments * all)));
